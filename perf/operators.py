@@ -250,7 +250,7 @@ def run(state):
     nll, lse = D.dbl_head_nll(s["h"], s["w"], s["x"])
     if kind == "nll":
         return dict(nll=nll, lse=lse)
-    dh, dw = D.dbl_head_nll_backward(s["h"], s["w"], s["x"], lse, s["g"], want_dw=s["dw"])
+    dh, dw = D.dbl_head_nll_backward(s["h"], s["w"], s["x"], nll, lse, s["g"], want_dw=s["dw"])
     return dict(nll=nll, lse=lse, dh=dh, dw=dw) if s["dw"] else dict(nll=nll, lse=lse, dh=dh)
 
 
