@@ -19,6 +19,9 @@
  *   dbl_expected_len    acceptance mass and expected accepted length along a given trajectory
  *   dbl_acceptance_objective  the training surrogate's forward quantities and the block NLL
  *   dbl_expand_branches / dbl_prior_head  the head's inputs: branch states and category logits
+ *   dbl_head_nll / dbl_head_nll_backward  the loss of given tokens under the head and its gradient
+ *   dbl_expand_branches_backward  gradients of the expander's weight, bias and trunk states
+ *   dbl_grad_norm / dbl_clip_grads  the global norm of a set of gradients, and clipping to it
  *   dbl_target_logprobs / dbl_early_determinism  the target side: the sampling transform that
  *                       defines p, and the target-block early-determinism estimate
  *
@@ -105,7 +108,11 @@ typedef enum {
   DBL_OP_SAMPLE_GREEDY = 4,
   DBL_OP_VERIFY_GREEDY = 5,
   DBL_OP_EXPECTED_LEN_GREEDY = 6,
-  DBL_OP_TARGET = 7              /* dbl_target_logprobs: rows N = shape.B * shape.K, shape.V */
+  DBL_OP_TARGET = 7,             /* dbl_target_logprobs: rows N = shape.B * shape.K, shape.V */
+  DBL_OP_HEAD_NLL = 16,
+  DBL_OP_HEAD_NLL_BACKWARD = 17,
+  DBL_OP_EXPAND_BACKWARD = 18,
+  DBL_OP_GRAD_NORM = 19          /* dbl_grad_norm: shape.B tensors (K = R = d = V = 1) */
 } dbl_op;
 
 typedef struct {
@@ -391,6 +398,96 @@ dbl_status dbl_target_logprobs(int64_t N, int64_t V, const float* logits, float 
  */
 dbl_status dbl_early_determinism(int64_t M, int64_t b, int64_t V, const int32_t* x,
                                  const float* logp, float* terms, float* mean, void* stream);
+
+/*
+ * dbl_head_nll - negative log-likelihood of given tokens under every branch, the term that the
+ * training losses are made of (Eq. block-nll: each row's -log q_k(x_k | y, z)), without the
+ * log-probabilities over the vocabulary:
+ *     logit = h w^T,  lse[b, k, z] = log sum_v exp(logit[b, k, z, v]),
+ *     nll[b, k, z] = lse[b, k, z] - logit[b, k, z, x[b, k]].
+ * A position whose token is outside [0, V) (padding, positions that are not trained on) does not
+ * count: its nll and lse are 0, its states are not looked at (they may hold anything) and it costs
+ * next to nothing. A row's results do not depend on the other rows of the call.
+ *   dt    DBL_BF16 (d % 8 == 0) or DBL_F32
+ *   h     [B, K, R, d] branch states;  w  [V, d] head weight, both of type dt
+ *   x     [B, K] int32 tokens
+ *   nll   out [B, K, R] fp32;  lse  out [B, K, R] fp32
+ *   ws    workspace of dbl_workspace_bytes(DBL_OP_HEAD_NLL, shape) bytes
+ * Errors: DBL_EINVAL for null or misaligned pointers, DBL_EDTYPE, DBL_ESHAPE (also for
+ * B*K*R >= 2^31), DBL_EWORKSPACE.
+ */
+dbl_status dbl_head_nll(dbl_shape shape, int dt, const void* h, const void* w, const int32_t* x,
+                        float* nll, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dbl_head_nll_backward - gradient of a loss L through dbl_head_nll: with g = dL/dnll and
+ * u[m, v] = exp(logit[m, v] - lse[m]) - [v = x[m]] for row m = (b, k, z),
+ *     dh[m] = g[m] sum_v u[m, v] w[v],      dw[v] = sum_m g[m] u[m, v] h[m],
+ * the logits formed again, a piece of the vocabulary at a time, and never kept whole. Positions that do
+ * not count (x outside [0, V)) get dh = 0 and add nothing to dw, whatever their h and g hold.
+ * fp32 accumulation; with bf16, u over (1 - p[x]) and h times g (1 - p[x]) are rounded to bf16 between
+ * the two matrix products, and the results once at the end.
+ *   nll, lse   as dbl_head_nll gave them for the same h, w and x
+ *   g     [B, K, R] fp32
+ *   dh    out [B, K, R, d] of type dt;  dw  out [V, d] of type dt, or NULL (the head is frozen)
+ *   ws    workspace of dbl_workspace_bytes(DBL_OP_HEAD_NLL_BACKWARD, shape) bytes (a piece of the
+ *         logits' gradient, up to about 1 GiB, and fp32 sums of dh)
+ * dh and dw may overlap neither each other nor an input. Errors: as dbl_head_nll.
+ */
+dbl_status dbl_head_nll_backward(dbl_shape shape, int dt, const void* h, const void* w,
+                                 const int32_t* x, const float* nll, const float* lse, const float* g,
+                                 void* dh, void* dw, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dbl_expand_branches_backward - gradients through dbl_expand_branches, from the gradient of the
+ * branch states (the dh of dbl_head_nll_backward):
+ *     dh[b, k]   = sum_z (dout[b, k, z] + W_z^T dout[b, k, z]),
+ *     dW[z*d + i, j] = sum_{b,k} dout[b, k, z, i] h[b, k, j],   dc[z*d + i] = sum_{b,k} dout[b, k, z, i]
+ * with fp32 accumulation, each rounded once to bf16.
+ *   shape   B, K, R, d used (V unused); d % 32 == 0, R*d <= 2^23
+ *   h       [B, K, d] bf16 trunk states;  W  [R*d, d] bf16;  dout  [B, K, R, d] bf16
+ *   dh      out [B, K, d] bf16 or NULL;  dW  out [R*d, d] bf16 or NULL;  dc  out [R*d] bf16 or NULL
+ *   ws      workspace of dbl_workspace_bytes(DBL_OP_EXPAND_BACKWARD, shape) bytes (V = 1), needed for dh;
+ *           otherwise may be 0 and NULL
+ * The outputs may overlap neither each other nor an input. B = 0 sets dW and dc to 0.
+ * Errors: DBL_EINVAL for null inputs, misaligned pointers or no output; DBL_ESHAPE; DBL_EWORKSPACE.
+ */
+dbl_status dbl_expand_branches_backward(dbl_shape shape, const void* h, const void* W,
+                                        const void* dout, void* dh, void* dW, void* dc, void* ws,
+                                        size_t ws_bytes, void* stream);
+
+/*
+ * dbl_grad_norm - Euclidean norm of n tensors taken together (the gradients of all parameters),
+ *     norm = sqrt(sum_i sum_j grads[i][j]^2),
+ * squares and sums in binary64. The three arrays are host memory, read during the call only; a call
+ * that is captured into a graph keeps the addresses in the graph.
+ *   n       number of tensors, 0 .. 2^20 (0: norm = 0)
+ *   grads   [n] device pointers, aligned to their elements (a view into a bucket may start
+ *           anywhere); a tensor of 0 elements may be NULL
+ *   numel   [n] numbers of elements >= 0, less than 2^44 together
+ *   dt      [n] DBL_F32 or DBL_BF16
+ *   norm    out: one fp32 (device)
+ *   ws      workspace of dbl_workspace_bytes(DBL_OP_GRAD_NORM, shape) bytes, shape.B = n and 1 elsewhere
+ * Errors: DBL_EINVAL, DBL_ESHAPE, DBL_EDTYPE, DBL_EWORKSPACE.
+ */
+dbl_status dbl_grad_norm(int64_t n, const void* const* grads, const int64_t* numel,
+                         const int32_t* dt, float* norm, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * dbl_clip_grads - gradients scaled to a largest global norm:
+ *     out[i][j] = grads[i][j] * min(1, max_norm / (norm + 1e-6)),
+ * computed in fp32 and rounded once. A norm that is not finite (an infinity or NaN among the gradients)
+ * is not hidden: an infinite one scales by 0, a NaN one gives NaN everywhere.
+ *   n, grads, numel, dt   as dbl_grad_norm
+ *   out       [n] device pointers of the same types and sizes, or NULL: in place. out[i] is grads[i] or
+ *             overlaps no gradient and no other output
+ *   norm      one fp32 (device), for example dbl_grad_norm's (of several devices' parts together)
+ *   max_norm  >= 0 (infinity: no limit)
+ * Errors: as dbl_grad_norm, and DBL_EINVAL for overlapping tensors or max_norm < 0 or NaN.
+ */
+dbl_status dbl_clip_grads(int64_t n, const void* const* grads, void* const* out,
+                          const int64_t* numel, const int32_t* dt, const float* norm,
+                          float max_norm, void* stream);
 
 /*
  * dbl_stream_read_probe - a diagnostic, not an operation of the method: reads every 16-byte

@@ -29,6 +29,9 @@ SOURCES = {
     "objective.hip": [],
     "target.hip": ["-ffp-contract=off"],
     "diag.hip": [],
+    "abi_train.hip": [],
+    "train.hip": [],
+    "clip.hip": [],
 }
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

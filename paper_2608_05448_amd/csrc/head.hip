@@ -307,6 +307,130 @@ __device__ __forceinline__ void tile_logsoftmax_store_lds(f32x16 (&acc)[NRB][NCB
   }
 }
 
+// What a GEMM kernel does with its accumulators (rows of w on the MFMA rows, rows of h on the
+// columns): the head's tile log-softmax (with or without the argmax keys), the category expander's
+// branch states, the training head's tile log-mass and token logit, or the logits' gradient.
+enum EpiKind : int {
+  kEpiLogSoftmax = 0,
+  kEpiLogSoftmaxArgmax = 1,
+  kEpiExpand = 2,
+  kEpiNll = 3,
+  kEpiGrad = 4
+};
+
+struct EpiArgs {
+  float* tls;            // head: [M, V]
+  float* lmass;          // head, nll: [M, nT]
+  uint64_t* amax;        // head: [M] argmax keys (argmax epilogue)
+  int nT, vec4;
+  __bf16* out;           // expander: [M, V] branch states, V = R * d
+  const __bf16* bias;    // expander: [V]
+  const __bf16* hres;    // expander: [M, d] trunk states (the residual)
+  int dres;              // expander: d
+  const int32_t* count;  // nll, grad: number of rows that count (M is the most there can be)
+  const TrainRow* rows;  // nll, grad: [M]
+  float* tgt;            // nll: [M] the token's logit
+  void* grad;            // grad: [M, ldg] the logits' gradient over this piece of the vocabulary
+  int64_t ldg;
+  int64_t vbase;         // grad: first id of the piece, a multiple of 256
+};
+
+constexpr bool epi_train(int epi) { return epi == kEpiNll || epi == kEpiGrad; }
+
+// Epilogue of dbl_head_nll: tile log-mass as in the head's epilogues (the same arithmetic as
+// tile_logsoftmax_store_lds), and the token's logit from the one lane that holds it.
+template <int NRB, int NCB>
+__device__ __forceinline__ void tile_nll_store(f32x16 (&acc)[NRB][NCB], const EpiArgs& e, int64_t M,
+                                               int64_t V, int64_t v0w, int64_t m0w, int lane) {
+  const int half = lane >> 5;
+  const int lim = static_cast<int>(V - v0w < kVTile ? V - v0w : kVTile) - 4 * half;
+#pragma unroll
+  for (int cb = 0; cb < NCB; ++cb) {
+    const int64_t m = m0w + cb * 32 + (lane & 31);
+    float x[NRB * 16];  // x[16 rb + r]: id 32 rb + 8 (r / 4) + 4 half + r % 4 of the tile
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        x[16 * rb + r] = 32 * rb + 8 * (r >> 2) + (r & 3) < lim ? acc[rb][cb][r] : -INFINITY;
+    // The token's offset in the tile, less this lane's 4 half (ids of this lane: bit 2 clear).
+    const int64_t o = m < M ? e.rows[m].token - v0w - 4 * half : -1;
+    if (o >= 0 && o < lim && !(o & 4)) {
+      float t = 0.0f;
+#pragma unroll
+      for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          t = o == 32 * rb + 8 * (r >> 2) + (r & 3) ? x[16 * rb + r] : t;
+      e.tgt[m] = t;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < NRB * 16; ++i) mx = fmaxf(mx, x[i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 32));
+    const float nb = -mx * kLog2e;
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NRB * 16; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, nb));
+    s += __shfl_xor(s, 32);
+    if (m < M && half == 0) e.lmass[m * e.nT + v0w / kVTile] = mx + __logf(s);
+  }
+}
+
+// Epilogue of dbl_head_nll_backward: the logits' gradient of a row over its scale, in bf16 (see
+// TrainRow): exp(logit - lse) / q for every id but the token, -1 for the token; 0 for the ids of a tile past V. With xp (8 KB of LDS of this wave) 32
+// rows x 128 ids at a time go through LDS, so that a store instruction writes four whole 256-byte row
+// segments (16-byte chunk c of row r at chunk c ^ (r % 16)); without, 8 bytes a lane.
+template <int NRB, int NCB, bool LDS>
+__device__ __forceinline__ void tile_grad_store(f32x16 (&acc)[NRB][NCB], const EpiArgs& e, int64_t M,
+                                                int64_t V, int64_t v0w, int64_t m0w, int lane,
+                                                char* xp) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  const int half = lane >> 5;
+  const int lr = lane & 31;
+  const int lim = static_cast<int>(V - v0w < kVTile ? V - v0w : kVTile) - 4 * half;
+  __bf16* const grad = static_cast<__bf16*>(e.grad);
+#pragma unroll
+  for (int cb = 0; cb < NCB; ++cb) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int64_t m = m0w + cb * 32 + lr;
+    const TrainRow row = e.rows[m < M ? m : M - 1];
+    const int64_t o = row.token - e.vbase - v0w - 4 * half;
+#pragma unroll
+    for (int rb = 0; rb < NRB; ++rb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        bf16x4 y;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int at = 32 * rb + 8 * g + q;
+          float p = __builtin_amdgcn_exp2f(fmaf(acc[rb][cb][4 * g + q], kLog2e, -row.shift));
+          p = o == at ? row.at_token : p;
+          y[q] = static_cast<__bf16>(at < lim ? p : 0.0f);
+        }
+        if constexpr (LDS)
+          *reinterpret_cast<bf16x4*>(xp + lr * 256 + (((rb * 4 + g) ^ (lr & 15)) * 16) + half * 8) = y;
+        else if (m < M)
+          *reinterpret_cast<bf16x4*>(grad + m * e.ldg + v0w + 32 * rb + 8 * g + 4 * half) = y;
+      }
+    if constexpr (LDS) {
+      // Wave-private LDS region: the writes above precede these reads in the wave's LDS queue.
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int jj = 0; jj < 8; ++jj) {
+        const int rr = 4 * jj + (lane >> 4);
+        const u32x4 y =
+            *reinterpret_cast<const u32x4*>(xp + rr * 256 + (((lane & 15) ^ (rr & 15)) * 16));
+        const int64_t mm = m0w + cb * 32 + rr;
+        if (mm < M) *reinterpret_cast<u32x4*>(grad + mm * e.ldg + v0w + 8 * (lane & 15)) = y;
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  }
+}
+
 // Tile configuration of the bf16 head kernel.
 //   BV x BM   vocabulary rows x branch rows per workgroup
 //   BK        hidden-dimension slice staged in LDS per step (double-buffered)
@@ -366,11 +490,10 @@ __device__ __forceinline__ void tile_of(int L, int n_vtiles, int n_mtiles, int* 
   }
 }
 
-template <class C, bool ARG>
+template <class C, int EPI>
 __global__ __launch_bounds__(C::kThreads, 1) void head_bf16_kernel(
-    const __bf16* __restrict__ h, const __bf16* __restrict__ w, float* __restrict__ tls,
-    float* __restrict__ lmass, uint64_t* __restrict__ amax, int64_t M, int64_t V, int d, int nT,
-    int n_mtiles, int vec4) {
+    const __bf16* __restrict__ h, const __bf16* __restrict__ w, const EpiArgs ea, int64_t M,
+    int64_t V, int d, int n_mtiles) {
   __shared__ __attribute__((aligned(16))) __bf16 As[2][C::BV * C::LDK];
   __shared__ __attribute__((aligned(16))) __bf16 Bs[2][C::BM * C::LDK];
 
@@ -384,6 +507,10 @@ __global__ __launch_bounds__(C::kThreads, 1) void head_bf16_kernel(
   tile_of(xcd_remap(blockIdx.x, gridDim.x), gridDim.x / n_mtiles, n_mtiles, &vt, &mt);
   const int64_t v0 = static_cast<int64_t>(vt) * C::BV;
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
+  if constexpr (epi_train(EPI)) {
+    M = *ea.count;
+    if (m0 >= M) return;
+  }
 
   // Staging: thread chunk c -> row c / CPR, 16-byte column c % CPR.
   const __bf16* a_src[C::A_CHUNKS];
@@ -495,8 +622,13 @@ __global__ __launch_bounds__(C::kThreads, 1) void head_bf16_kernel(
 
   const int64_t v0w = v0 + wv * kVTile;
   if (v0w >= V) return;
-  tile_logsoftmax_store<C::NRB, C::NCB, ARG>(acc, tls, lmass, amax, M, V, nT, v0w,
-                                             m0 + wm * C::TM, lane, vec4);
+  if constexpr (EPI == kEpiNll)
+    tile_nll_store<C::NRB, C::NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
+  else if constexpr (EPI == kEpiGrad)
+    tile_grad_store<C::NRB, C::NCB, false>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, nullptr);
+  else
+    tile_logsoftmax_store<C::NRB, C::NCB, EPI == kEpiLogSoftmaxArgmax>(
+        acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane, ea.vec4);
 }
 
 // Every kernel that can serve a shape adds a row's products in the same order, 16 hidden units at a
@@ -608,22 +740,6 @@ __device__ __forceinline__ void wait_vmcnt() {
 #endif
 using DCfg = DmaCfg<DBL_HEAD_BK, DBL_HEAD_STAGES, DBL_HEAD_BM, DBL_HEAD_WM>;
 
-// What the direct-to-LDS GEMM does with its accumulators (rows of w on the MFMA rows, rows of h
-// on the columns): the head's tile log-softmax (with or without the argmax keys), or the
-// category expander's branch states.
-enum EpiKind : int { kEpiLogSoftmax = 0, kEpiLogSoftmaxArgmax = 1, kEpiExpand = 2 };
-
-struct EpiArgs {
-  float* tls;            // head: [M, V]
-  float* lmass;          // head: [M, nT]
-  uint64_t* amax;        // head: [M] argmax keys (argmax epilogue)
-  int nT, vec4;
-  __bf16* out;           // expander: [M, V] branch states, V = R * d
-  const __bf16* bias;    // expander: [V]
-  const __bf16* hres;    // expander: [M, d] trunk states (the residual)
-  int dres;              // expander: d
-};
-
 // Expander epilogue: out[m, v] = bf16(h[m, v mod d] + (acc + c[v])), i.e. h_{k,z} = h_k + g_z(h_k)
 // with g_z(h) = W_z h + c_z evaluated in fp32 and rounded once. Lane l holds row
 // m0w + 32 cb + l % 32 and, in registers 4g..4g+3 of row block rb, the four consecutive features
@@ -687,6 +803,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWgPerCu) void head_bf16_dma_kernel
   tile_of(xcd_remap(blockIdx.x, gridDim.x), gridDim.x / n_mtiles, n_mtiles, &vt, &mt);
   const int64_t v0 = static_cast<int64_t>(vt) * C::BV;
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
+  if constexpr (epi_train(EPI)) {
+    M = *ea.count;
+    if (m0 >= M) return;
+  }
 
   // DMA sources: instruction i of this wave covers tile rows (wave * INST + i) * RPI + [0, RPI);
   // lane -> row lane / CPR of it and the chunk whose permuted slot is lane % CPR. Addresses are
@@ -852,6 +972,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWgPerCu) void head_bf16_dma_kernel
   if (v0w >= V) return;
   if constexpr (EPI == kEpiExpand)
     expand_store<C::NRB, C::NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
+  else if constexpr (EPI == kEpiNll)
+    tile_nll_store<C::NRB, C::NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
+  else if constexpr (EPI == kEpiGrad)
+    tile_grad_store<C::NRB, C::NCB, false>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, nullptr);
   else
     tile_logsoftmax_store<C::NRB, C::NCB, EPI == kEpiLogSoftmaxArgmax>(
         acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane, ea.vec4);
@@ -1129,7 +1253,7 @@ __device__ __forceinline__ void pp_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <bool ARG>
+template <int EPI>
 __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
     const __bf16* __restrict__ h, const __bf16* __restrict__ w, const EpiArgs ea, int64_t M,
     int64_t V, int d, int n_mtiles) {
@@ -1149,6 +1273,10 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
   tile_of(xcd_remap(blockIdx.x, gridDim.x), gridDim.x / n_mtiles, n_mtiles, &vt, &mt);
   const int64_t v0 = static_cast<int64_t>(vt) * C::BV;
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
+  if constexpr (epi_train(EPI)) {
+    M = *ea.count;
+    if (m0 >= M) return;
+  }
 
   // Copies: wave q of group g copies rows 128 g + (4 q + i) * 8 + lane / 8 (i < 4) of the w tile
   // and of the h tile; lane % 8 is its 16-byte chunk's place in the LDS row and it fetches
@@ -1168,7 +1296,7 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
   }
   const uint32_t lds_row = lds_addr(smem) + (16 * grp + 4 * q) * 1024;
   const int nk = d / C::BK;
-  const int k0 = walk_start<false>(v0, d) / C::BK;
+  const int k0 = walk_start<false>(EPI == kEpiGrad ? v0 + ea.vbase : v0, d) / C::BK;
   auto copy_A = [&](int s, int slot) {
     s = s + k0 < nk ? s + k0 : s + k0 - nk;
     const char* base = srcA + static_cast<int64_t>(s) * (2 * C::BK);
@@ -1275,8 +1403,14 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
   // its stores in its own 16 KB of them.
   const int64_t v0w = v0 + wv * kVTile;
   if (v0w >= V) return;
-  tile_logsoftmax_store_lds<NRB, NCB, ARG>(acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w,
-                                           m0 + wm * C::TM, lane, smem + wave * 16384);
+  if constexpr (EPI == kEpiNll)
+    tile_nll_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
+  else if constexpr (EPI == kEpiGrad)
+    tile_grad_store<NRB, NCB, true>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 16384);
+  else
+    tile_logsoftmax_store_lds<NRB, NCB, EPI == kEpiLogSoftmaxArgmax>(
+        acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane,
+        smem + wave * 16384);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1322,6 +1456,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
   tile_of(xcd_remap(blockIdx.x, gridDim.x), gridDim.x / n_mtiles, n_mtiles, &vt, &mt);
   const int64_t v0 = static_cast<int64_t>(vt) * C::BV;
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
+  if constexpr (epi_train(EPI)) {
+    M = *ea.count;
+    if (m0 >= M) return;
+  }
 
   // Each copy instruction covers 8 rows of a block: wave q copies the row groups q AW .. q AW + AW - 1
   // of the weight rows and q BW .. of the branch rows; lane -> row lane / 8 of the group and the
@@ -1344,7 +1482,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
   }
   const uint32_t lds0 = lds_addr(smem);
   const int nk = d / (64 * C::KB);
-  const int r0 = walk_start<EPI == kEpiExpand>(v0, d) / (64 * C::KB);
+  const int r0 = walk_start<EPI == kEpiExpand>(EPI == kEpiGrad ? v0 + ea.vbase : v0, d) / (64 * C::KB);
   auto copy = [&](int s, int slot) {
     s = s + r0 < nk ? s + r0 : s + r0 - nk;
     const uint32_t to = lds0 + slot * C::STAGE;
@@ -1415,6 +1553,11 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
   if (v0w >= V) return;
   if constexpr (EPI == kEpiExpand) {
     expand_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
+  } else if constexpr (EPI == kEpiNll) {
+    tile_nll_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
+  } else if constexpr (EPI == kEpiGrad) {
+    static_assert(C::NW * 8192 <= C::kLds, "8 KB of the ring per wave that stores");
+    tile_grad_store<NRB, NCB, true>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 8192);
   } else {
     static_assert(C::TV == kVTile && C::WV * C::WM * 16384 <= C::kLds,
                   "head epilogue: 16 KB of the ring per wave that stores");
@@ -1625,7 +1768,56 @@ hipError_t launch_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64
   return hipGetLastError();
 }
 
+// The head's GEMM with the kernel that its shape takes.
+template <int EPI>
+hipError_t launch_head_gemm(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64_t M, int64_t V,
+                            int d, hipStream_t stream) {
+  // Up to 128 rows the weight's stream bounds the call and a 256-row tile would be mostly padding.
+  // V = 151,936, with the LSE launch: 60 rows at d = 2560 203 -> 149 us, 120 rows 212 -> 176, 60 rows
+  // at d = 4096 300 -> 217, 120 rows 306 -> 242; from 129 rows on two 128-row tiles would stream the
+  // weight twice (180 rows at d = 2560 264 us against the ping-pong kernel's 215).
+  if (d % 64 == 0 && M <= 128) {
+    return M > HeadFew64::BM ? launch_few<HeadFew128, EPI>(h, w, ea, M, V, d, stream)
+           : (V + HeadFew64::BV - 1) / HeadFew64::BV >= kFewTiles
+               ? launch_few<HeadFew64, EPI>(h, w, ea, M, V, d, stream)
+               : launch_few<HeadFew64Short, EPI>(h, w, ea, M, V, d, stream);
+  }
+  static_assert(PpCfg::BM == 256 && PpCfg::BV == 256 && DCfg::BM == 256 && DCfg::BV == 256 &&
+                    Cfg::BM == 256 && Cfg::BV == 256, "one grid for the 256 x 256 tiles");
+  const int64_t dm = (M + 255) / 256;
+  const int64_t nwg = ((V + 255) / 256) * dm;
+  if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
+  const dim3 grid(static_cast<unsigned>(nwg));
+  const int n_mtiles = static_cast<int>(dm);
+  if (d % PpCfg::BK == 0)
+    hipLaunchKernelGGL(head_bf16_pp_kernel<EPI>, grid, dim3(PpCfg::kThreads), 0, stream, h, w, ea, M,
+                       V, d, n_mtiles);
+  else if (d % DCfg::BK == 0)
+    hipLaunchKernelGGL((head_bf16_dma_kernel<DCfg, EPI>), grid, dim3(DCfg::kThreads), 0, stream, h, w,
+                       ea, M, V, d, n_mtiles);
+  else
+    hipLaunchKernelGGL((head_bf16_kernel<Cfg, EPI>), grid, dim3(Cfg::kThreads), 0, stream, h, w, ea,
+                       M, V, d, n_mtiles);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_head_train(const HeadTrainArgs& a, bool grad, hipStream_t stream) {
+  EpiArgs ea{};
+  ea.lmass = a.lmass;
+  ea.nT = static_cast<int>((a.V + kVTile - 1) / kVTile);
+  ea.count = a.count;
+  ea.rows = a.rows;
+  ea.tgt = a.tgt;
+  ea.grad = a.grad;
+  ea.ldg = a.ldg;
+  ea.vbase = a.vbase;
+  const __bf16* h = static_cast<const __bf16*>(a.h);
+  const __bf16* w = static_cast<const __bf16*>(a.w);
+  return grad ? launch_head_gemm<kEpiGrad>(h, w, ea, a.M, a.V, a.d, stream)
+              : launch_head_gemm<kEpiNll>(h, w, ea, a.M, a.V, a.d, stream);
+}
 
 hipError_t launch_head(const HeadArgs& a, hipStream_t stream) {
   const int nT = static_cast<int>((a.V + kVTile - 1) / kVTile);
@@ -1639,76 +1831,18 @@ hipError_t launch_head(const HeadArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   if (a.dtype_bf16) {
-    const int n_mtiles = static_cast<int>((a.M + Cfg::BM - 1) / Cfg::BM);
-    const int64_t n_vtiles = (a.V + Cfg::BV - 1) / Cfg::BV;
-    const int64_t nwg = n_vtiles * n_mtiles;
-    if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
-    const int vec4 = (a.V % 4 == 0) ? 1 : 0;
+    EpiArgs ea{};
+    ea.tls = a.tls;
+    ea.lmass = a.lmass;
+    ea.amax = amax;
+    ea.nT = nT;
+    ea.vec4 = (a.V % 4 == 0) ? 1 : 0;
     const __bf16* h = static_cast<const __bf16*>(a.h);
     const __bf16* w = static_cast<const __bf16*>(a.w);
-    // Up to 128 rows the weight's stream bounds the call and a 256-row tile would be mostly padding.
-    // V = 151,936, with the LSE launch: 60 rows at d = 2560 203 -> 149 us, 120 rows 212 -> 176, 60 rows
-    // at d = 4096 300 -> 217, 120 rows 306 -> 242; from 129 rows on two 128-row tiles would stream the
-    // weight twice (180 rows at d = 2560 264 us against the ping-pong kernel's 215).
-    if (a.d % 64 == 0 && a.M <= 128) {
-      EpiArgs ea{};
-      ea.tls = a.tls;
-      ea.lmass = a.lmass;
-      ea.amax = amax;
-      ea.nT = nT;
-      auto few = [&](auto cfg) {
-        using C = decltype(cfg);
-        return amax ? launch_few<C, kEpiLogSoftmaxArgmax>(h, w, ea, a.M, a.V, a.d, stream)
-                    : launch_few<C, kEpiLogSoftmax>(h, w, ea, a.M, a.V, a.d, stream);
-      };
-      const hipError_t e = a.M > HeadFew64::BM ? few(HeadFew128{})
-                           : (a.V + HeadFew64::BV - 1) / HeadFew64::BV >= kFewTiles
-                               ? few(HeadFew64{})
-                               : few(HeadFew64Short{});
-      if (e != hipSuccess) return e;
-    } else if (a.d % PpCfg::BK == 0) {
-      const int dm = static_cast<int>((a.M + PpCfg::BM - 1) / PpCfg::BM);
-      const int64_t dwg = ((a.V + PpCfg::BV - 1) / PpCfg::BV) * dm;
-      if (dwg > 0x7fffffff) return hipErrorInvalidConfiguration;
-      EpiArgs ea{};
-      ea.tls = a.tls;
-      ea.lmass = a.lmass;
-      ea.amax = amax;
-      ea.nT = nT;
-      ea.vec4 = vec4;
-      const dim3 grid(static_cast<unsigned>(dwg)), block(PpCfg::kThreads);
-      if (amax)
-        hipLaunchKernelGGL(head_bf16_pp_kernel<true>, grid, block, 0, stream, h, w, ea, a.M, a.V,
-                           a.d, dm);
-      else
-        hipLaunchKernelGGL(head_bf16_pp_kernel<false>, grid, block, 0, stream, h, w, ea, a.M,
-                           a.V, a.d, dm);
-    } else if (a.d % DCfg::BK == 0) {
-      const int dm = static_cast<int>((a.M + DCfg::BM - 1) / DCfg::BM);
-      const int64_t dwg = ((a.V + DCfg::BV - 1) / DCfg::BV) * dm;
-      if (dwg > 0x7fffffff) return hipErrorInvalidConfiguration;
-      const dim3 grid(static_cast<unsigned>(dwg)), block(DCfg::kThreads);
-      EpiArgs ea{};
-      ea.tls = a.tls;
-      ea.lmass = a.lmass;
-      ea.amax = amax;
-      ea.nT = nT;
-      ea.vec4 = vec4;
-      if (amax)
-        hipLaunchKernelGGL((head_bf16_dma_kernel<DCfg, kEpiLogSoftmaxArgmax>), grid, block, 0,
-                           stream, h, w, ea, a.M, a.V, a.d, dm);
-      else
-        hipLaunchKernelGGL((head_bf16_dma_kernel<DCfg, kEpiLogSoftmax>), grid, block, 0, stream,
-                           h, w, ea, a.M, a.V, a.d, dm);
-    } else {
-      const dim3 grid(static_cast<unsigned>(nwg)), block(Cfg::kThreads);
-      if (amax)
-        hipLaunchKernelGGL((head_bf16_kernel<Cfg, true>), grid, block, 0, stream, h, w, a.tls,
-                           a.lmass, amax, a.M, a.V, a.d, nT, n_mtiles, vec4);
-      else
-        hipLaunchKernelGGL((head_bf16_kernel<Cfg, false>), grid, block, 0, stream, h, w, a.tls,
-                           a.lmass, amax, a.M, a.V, a.d, nT, n_mtiles, vec4);
-    }
+    const hipError_t e =
+        amax ? launch_head_gemm<kEpiLogSoftmaxArgmax>(h, w, ea, a.M, a.V, a.d, stream)
+             : launch_head_gemm<kEpiLogSoftmax>(h, w, ea, a.M, a.V, a.d, stream);
+    if (e != hipSuccess) return e;
   } else {
     const int64_t m16 = (a.M + 15) / 16, m4 = (a.M + 3) / 4;
     const bool wide = f32_rows16(a.M, a.d, nT);

@@ -143,6 +143,112 @@ struct DeterminismArgs {
   float* mean;          // scalar or null
 };
 
+// One row that is trained on, as the head's training kernels see it. The gradient of its negative
+// log-likelihood with respect to the logits, g (p_v - [v = token]), is handled as scale * u_v with
+// u_v = exp(logit_v - shift') (shift' = lse + ln q) and u = at_token at the token.
+// bf16: q = 1 - p_token = -expm1(-nll), scale = g q, so that u is -1 at the token (exact in bf16) and in
+// [0, 1] elsewhere: the rounding of u to bf16 then touches the other ids only, whose errors average out,
+// and never the one entry that most of the gradient rests on. q is kept from below by 2^-24, the rounding
+// of a binary32 probability near 1 (at_token = -(1 - p) / q there). fp32: q = 1.
+struct alignas(16) TrainRow {
+  float shift;     // bf16: (lse + ln q) log2(e); fp32: lse
+  float at_token;
+  float scale;
+  int32_t token;
+};
+
+// The training head's GEMM over the rows that count (bf16): tile log-masses and token logits, or the
+// scaled logits' gradient u over a piece of the vocabulary.
+struct HeadTrainArgs {
+  int64_t M;             // rows there can be
+  int64_t V;             // ids of w (of the piece)
+  int d;
+  const void* h;         // [M, d] rows that count first
+  const void* w;         // [V, d]
+  const int32_t* count;  // rows that count
+  const TrainRow* rows;  // [M]
+  float* lmass;          // nll: [M, nT]
+  float* tgt;            // nll: [M]
+  void* grad;            // gradient: [M, ldg]
+  int64_t ldg, vbase;
+};
+
+// dbl_head_nll and its gradient; workspace pointers are carved out by the ABI.
+struct NllArgs {
+  int64_t P, R, V;       // positions, categories
+  int d;
+  bool bf16;
+  const void* h;         // [P, R, d]
+  const void* w;         // [V, d]
+  const int32_t* x;      // [P]
+  float* nll;            // [P, R] out (backward: in)
+  float* lse;            // [P, R] out (backward: in)
+  const float* g;        // backward: [P, R]
+  void* dh;              // backward: [P, R, d]
+  void* dw;              // backward: [V, d] or null
+  void* hc;              // workspace [M, d]: rows that count
+  void* hs;              // workspace [M, d]: the same times their scale (dw)
+  TrainRow* rows;        // workspace [M]
+  int32_t* inv;          // workspace [P]: place of a position among those that count, or -1
+  int32_t* count;        // workspace
+  float* lmass;          // workspace [M, nT]
+  float* tgt;            // workspace [M]
+  void* grad;            // workspace [M, piece]
+  float* part;           // workspace [splits, M, d]
+  int64_t piece;         // ids per piece, a multiple of 256
+  int splits;
+};
+
+struct ExpandBackwardArgs {
+  int64_t P, R;
+  int d;
+  const void* h;         // [P, d]
+  const void* W;         // [R*d, d]
+  const void* dout;      // [P, R*d]
+  void* dh;              // [P, d] or null
+  void* dW;              // [R*d, d] or null
+  void* dc;              // [R*d] or null
+  float* part;           // workspace [splits, P, d]
+  int splits;
+};
+
+// One tensor of a set of gradients.
+struct GradTensor {
+  const void* g;
+  void* out;             // clipping only
+  int64_t n;
+  int32_t bf16;
+};
+
+// Ids of the vocabulary that the head's backward pass takes at a time: as many as give a gradient of
+// about 1 GiB, at least 8192, in equal pieces of a multiple of 4096.
+constexpr int64_t kPieceBytes = int64_t(1) << 30;
+inline int64_t nll_piece(int64_t M, int64_t V, int elem) {
+  const int64_t most = kPieceBytes / (elem * (M > 0 ? M : 1));
+  const int64_t cap = most < 8192 ? 8192 : most / 4096 * 4096;
+  const int64_t pieces = (V + cap - 1) / cap;
+  const int64_t each = (V + pieces - 1) / pieces;
+  return (each + 4095) / 4096 * 4096;
+}
+
+// How many parts the sum over K of an [nb, na] product is split into, so that `tile` x `tile` output
+// tiles times parts fill the chip (a part has 256 terms at least).
+inline int grad_splits(int64_t na, int64_t nb, int64_t K) {
+  const int64_t tiles = ((na + 127) / 128) * ((nb + 127) / 128);
+  if (tiles == 0) return 1;
+  int64_t s = (512 + tiles - 1) / tiles;
+  const int64_t most = (K + 255) / 256;
+  s = s < most ? s : most;
+  return static_cast<int>(s < 1 ? 1 : s);
+}
+
+constexpr int64_t kMaxTrainRows = 0x7fffffff;
+
+constexpr int kNormSet = 180;      // tensors of one launch of the gradient norm
+constexpr int kNormBlocks = 1024;  // its workgroups, and partial sums, at most
+inline int64_t norm_parts(int64_t n) { return (n + kNormSet - 1) / kNormSet * kNormBlocks; }
+constexpr int64_t kMaxGradElements = int64_t(1) << 44;  // of all tensors (chunks are numbered in 31 bits)
+
 inline int n_chunks(int nT) { return (nT + kTilesPerChunk - 1) / kTilesPerChunk; }
 
 hipError_t launch_head(const HeadArgs& a, hipStream_t stream);
@@ -153,6 +259,14 @@ hipError_t launch_verify_greedy(const GreedyArgs& a, hipStream_t stream);
 hipError_t launch_objective(const ObjectiveArgs& a, hipStream_t stream);
 hipError_t launch_expand(const ExpandArgs& a, hipStream_t stream);
 hipError_t launch_prior_head(const PriorHeadArgs& a, hipStream_t stream);
+hipError_t launch_head_train(const HeadTrainArgs& a, bool grad, hipStream_t stream);
+hipError_t launch_nll(const NllArgs& a, hipStream_t stream);
+hipError_t launch_nll_backward(const NllArgs& a, hipStream_t stream);
+hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t stream);
+hipError_t launch_grad_norm(const GradTensor* t, int64_t n, double* part, float* norm,
+                            hipStream_t stream);
+hipError_t launch_clip_grads(const GradTensor* t, int64_t n, const float* norm, float max_norm,
+                             hipStream_t stream);
 hipError_t launch_filter(const FilterArgs& a, hipStream_t stream);
 hipError_t launch_determinism(const DeterminismArgs& a, hipStream_t stream);
 hipError_t launch_read_probe(const void* buf, int64_t bytes, float* partials, int64_t n_partials,

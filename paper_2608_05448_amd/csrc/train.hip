@@ -1,0 +1,971 @@
+// Training: the negative log-likelihood of given tokens under the LM head and its gradient, and the
+// backward pass of the branch expander.
+//
+// Head. A row's loss is nll = lse - logit[token]; its gradient with respect to the logits is
+// u = p - [v = token] times the loss's gradient g, and dh = (g u) w, dw = (g u)^T h. The logits are
+// never kept: the forward pass reduces them in the head GEMM's epilogue, the backward pass forms them
+// again, a piece of the vocabulary at a time, as u in bf16 (fp32 for fp32 inputs), which the two
+// products then read.
+// Rows whose token is outside [0, V) do not count: the rows that do are gathered first, so that the
+// others cost nothing and whatever they hold (NaN, infinities) reaches no result.
+//
+// Products. Both operands of the products meet along a dimension that at least one of them does not
+// hold contiguously ([K, n] row-major). Such an operand is copied to LDS as it lies and its MFMA
+// fragments are read with the transposing LDS reads (ds_read_b64_tr_b16). The output's contiguous
+// dimension lies on the MFMA rows, so that a lane holds four consecutive outputs.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "kernels.hpp"
+
+namespace dbl {
+namespace {
+
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// ---------------------------------------------------------------------------------------
+// Rows that count.
+
+__device__ __forceinline__ bool counts(int32_t x, int64_t V) { return x >= 0 && x < V; }
+
+__device__ __forceinline__ int wave_sum_int(int v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+
+// Up to this many positions every workgroup of the gather counts the positions before its own itself
+// (at most 16 KB from L2); beyond, one workgroup counts them all first.
+constexpr int64_t kCountInline = 4096;
+
+__global__ __launch_bounds__(1024) void count_positions_kernel(const int32_t* __restrict__ x, int64_t P,
+                                                               int R, int64_t V,
+                                                               int32_t* __restrict__ inv,
+                                                               int32_t* __restrict__ count) {
+  __shared__ int part[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0;
+  for (int64_t p0 = 0; p0 < P; p0 += 1024) {
+    const int64_t p = p0 + threadIdx.x;
+    const bool c = p < P && counts(x[p], V);
+    const uint64_t mask = __ballot(c);
+    if (lane == 0) part[wave] = __popcll(mask);
+    __syncthreads();
+    int at = before, all = 0;
+    for (int i = 0; i < 16; ++i) {
+      at += i < wave ? part[i] : 0;
+      all += part[i];
+    }
+    at += __popcll(mask & ((uint64_t(1) << lane) - 1));
+    if (p < P) inv[p] = c ? at : -1;
+    before += all;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *count = before * R;
+}
+
+// One workgroup per position: its place among the positions that count, its R rows of h copied there
+// (and, for dw, times their scale), and what the head's kernels need of each row.
+template <class T>
+__global__ __launch_bounds__(256) void gather_rows_kernel(const NllArgs a, int counted) {
+  __shared__ int part[4];
+  __shared__ float scale[kMaxR];
+  const int64_t p = blockIdx.x;
+  const int R = static_cast<int>(a.R), d = a.d;
+  const int32_t token = a.x[p];
+  const bool mine = counts(token, a.V);
+  int at;
+  if (counted) {
+    at = a.inv[p];
+  } else {
+    int c = 0;
+    for (int64_t i = threadIdx.x; i < p; i += 256) c += counts(a.x[i], a.V) ? 1 : 0;
+    c = wave_sum_int(c);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = c;
+    __syncthreads();
+    at = part[0] + part[1] + part[2] + part[3];
+    if (threadIdx.x == 0) {
+      a.inv[p] = mine ? at : -1;
+      if (p == a.P - 1) *a.count = (at + (mine ? 1 : 0)) * R;
+    }
+  }
+  if (!mine) return;
+  const int64_t to = static_cast<int64_t>(at) * R;
+  if (static_cast<int>(threadIdx.x) < R) {
+    const int r = threadIdx.x;
+    TrainRow row{0.0f, 0.0f, 0.0f, token};
+    if (a.g) {
+      const float lse = a.lse[p * R + r], g = a.g[p * R + r];
+      const float q = -expm1f(-fmaxf(a.nll[p * R + r], 0.0f));
+      if (sizeof(T) == 2) {
+        const float qc = fmaxf(q, 0x1p-24f);
+        row.shift = (lse + logf(qc)) * kLog2e;
+        row.at_token = -q / qc;
+        row.scale = g * qc;
+      } else {
+        row.shift = lse;
+        row.at_token = -q;
+        row.scale = g;
+      }
+    }
+    a.rows[to + r] = row;
+    scale[r] = row.scale;
+  }
+  __syncthreads();
+  const T* src = static_cast<const T*>(a.h) + p * R * d;
+  T* dst = static_cast<T*>(a.hc) + to * d;
+  T* dss = a.hs ? static_cast<T*>(a.hs) + to * d : nullptr;
+  if (sizeof(T) == 2) {  // d % 8 == 0
+    for (int r = 0; r < R; ++r)
+      for (int j = 8 * threadIdx.x; j < d; j += 2048) {
+        const bf16x8 v = *reinterpret_cast<const bf16x8*>(src + static_cast<int64_t>(r) * d + j);
+        *reinterpret_cast<bf16x8*>(dst + static_cast<int64_t>(r) * d + j) = v;
+        if (dss) {
+          bf16x8 y;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) y[i] = static_cast<__bf16>(static_cast<float>(v[i]) * scale[r]);
+          *reinterpret_cast<bf16x8*>(dss + static_cast<int64_t>(r) * d + j) = y;
+        }
+      }
+  } else {
+    for (int r = 0; r < R; ++r)
+      for (int j = threadIdx.x; j < d; j += 256) {
+        const int64_t o = static_cast<int64_t>(r) * d + j;
+        const T v = src[o];
+        dst[o] = v;
+        if (dss) dss[o] = static_cast<T>(static_cast<float>(v) * scale[r]);
+      }
+  }
+}
+
+hipError_t gather_rows(const NllArgs& a, hipStream_t stream) {
+  const int counted = a.P > kCountInline;
+  if (counted)
+    hipLaunchKernelGGL(count_positions_kernel, dim3(1), dim3(1024), 0, stream, a.x, a.P,
+                       static_cast<int>(a.R), a.V, a.inv, a.count);
+  const dim3 grid(static_cast<unsigned>(a.P));
+  if (a.bf16)
+    hipLaunchKernelGGL(gather_rows_kernel<__bf16>, grid, dim3(256), 0, stream, a, counted);
+  else
+    hipLaunchKernelGGL(gather_rows_kernel<float>, grid, dim3(256), 0, stream, a, counted);
+  return hipGetLastError();
+}
+
+// lse and nll of every row from the tile log-masses; 0 for the rows that do not count. One wave a row.
+__global__ __launch_bounds__(256) void nll_finish_kernel(const NllArgs a, int nT) {
+  const int64_t m = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (m >= a.P * a.R) return;
+  const int at = a.inv[m / a.R];
+  float lse = 0.0f, nll = 0.0f;
+  if (at >= 0) {
+    const int64_t i = static_cast<int64_t>(at) * a.R + m % a.R;
+    const float* row = a.lmass + i * nT;
+    float mx = -INFINITY, s = 0.0f;
+    for (int t = lane; t < nT; t += 64) {  // running maximum and sum
+      const float v = row[t], top = fmaxf(mx, v);
+      s = top > -INFINITY ? s * expf(mx - top) + expf(v - top) : 0.0f;
+      mx = top;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const float omx = __shfl_xor(mx, o), os = __shfl_xor(s, o), top = fmaxf(mx, omx);
+      s = top > -INFINITY ? s * expf(mx - top) + os * expf(omx - top) : 0.0f;
+      mx = top;
+    }
+    lse = mx + logf(s);
+    nll = lse - a.tgt[i];
+  }
+  if (lane == 0) {
+    a.lse[m] = lse;
+    a.nll[m] = nll;
+  }
+}
+
+// ---------------------------------------------------------------------------------------
+// bf16 products out[b, a] = sum_k B(k, b) A[k, a] with A [K, lda] row-major.
+
+struct Prod {
+  const __bf16* A;       // [K, lda], columns na
+  const __bf16* B;       // TRB: [K, ldb], columns nb; else [nb, ldb], contiguous along K
+  int64_t lda, ldb, na, nb, K;
+  const int32_t* count;  // if set: K (TRB) or nb
+  float* part;           // [splits, nb_max, na] fp32 sums, or null
+  int64_t part_stride;   // elements between splits
+  int accumulate;        // add to what part holds
+  __bf16* out;           // [nb, na] bf16 (one split)
+  int splits;
+  int n_btiles;
+};
+
+__device__ __forceinline__ uint32_t lds_addr(const char* p) {
+  return static_cast<uint32_t>(
+      reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) char*)(p)));
+}
+
+// One global_load_lds_dwordx4 (lane i copies 16 bytes from sbase + voff to LDS byte m0 + 16 i), issued
+// through inline asm so that the compiler does not drain every outstanding copy before each LDS read;
+// completion is tracked with wait_vmcnt. The wait states cover a VALU write of the scalar base.
+__device__ __forceinline__ void lds_dma16(const char* sbase, uint32_t voff, uint32_t m0v) {
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(m0v)
+               : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ int xcd_remap(int id, int n) {
+  const int q = n >> 3, rem = n & 7;
+  const int x = id & 7, s = id >> 3;
+  return x < rem ? x * (q + 1) + s : rem * (q + 1) + (x - rem) * q + s;
+}
+
+// Four bf16 from each of the 16 lanes of a group, transposed: with lane i's address at row i / 4,
+// columns 4 (i % 4) .. + 3 of a 4 x 16 block, lane i receives column i, rows 0 .. 3.
+__device__ __forceinline__ s16x4 lds_read_tr(const char* p) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) s16x4*)(uintptr_t)(lds_addr(p)));
+}
+
+__device__ __forceinline__ bf16x8 join(s16x4 lo, s16x4 hi) {
+  typedef short s16x8 __attribute__((ext_vector_type(8)));
+  const s16x8 v = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  return __builtin_bit_cast(bf16x8, v);
+}
+
+// The first n (of 8) values of a fragment, the others 0.
+__device__ __forceinline__ bf16x8 keep_first(bf16x8 v, int n) {
+  u32x4 u = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    u[i] = n >= 2 * i + 2 ? u[i] : n == 2 * i + 1 ? (u[i] & 0xffffu) : 0u;
+  return __builtin_bit_cast(bf16x8, u);
+}
+
+// LDS layout of a transposed operand: row k of a stage holds C columns; 16-byte chunk c of row k lies
+// at chunk c ^ tr_swz(k), so that the four rows that a transposing read takes 64 bytes of each lie in
+// different banks.
+template <int C>
+__device__ __forceinline__ int tr_swz(int k) {
+  static_assert(C == 64 || C % 128 == 0, "columns per LDS row");
+  return C == 64 ? 4 * ((k >> 1) & 1) : 4 * (k & 3);
+}
+// LDS layout of an operand held along K: 128-byte rows, chunk c of row r at chunk c ^ ((r / 2) % 8).
+__device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
+
+// Ring kernel: BA x BB output tile, WA x WB waves, 64-deep stages copied global -> LDS into an S-slot
+// ring S - 1 stages ahead, one barrier per stage.
+template <int BA_, int BB_, int WA_, int WB_, int S_>
+struct RingCfg {
+  static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = WB_, S = S_;
+  static constexpr int NW = WA * WB, kThreads = 64 * NW;
+  static constexpr int NRA = BA / WA / 32, NCB = BB / WB / 32;
+  static constexpr int TILEA = BA * 128, TILEB = BB * 128, STAGE = TILEA + TILEB;
+  static constexpr int AI = TILEA / 1024 / NW, BI = TILEB / 1024 / NW;  // copies per wave and stage
+  static constexpr int PER = AI + BI;
+  static constexpr int kLds = S * STAGE;
+  static constexpr int kWgPerCu = 160 * 1024 / kLds;
+  static constexpr int kWavesPerEu = kWgPerCu * NW < 8 ? 1 : kWgPerCu * NW < 16 ? 2 : 4;
+  static_assert(TILEA % (1024 * NW) == 0 && TILEB % (1024 * NW) == 0, "whole copies");
+  static_assert(NRA >= 1 && NCB >= 1 && BA % (32 * WA) == 0 && BB % (32 * WB) == 0, "tiling");
+  static_assert((S - 1) * PER <= 63 && kLds <= 160 * 1024, "ring");
+};
+
+template <class C, bool TRB, bool PART>
+__global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(const Prod p) {
+  constexpr int BA = C::BA, BB = C::BB, NRA = C::NRA, NCB = C::NCB;
+  __shared__ __attribute__((aligned(1024))) char smem[C::kLds];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wa = wave / C::WB, wb = wave % C::WB;
+
+  int64_t K = p.K, nb = p.nb;
+  if (p.count) {
+    if (TRB) K = *p.count;
+    else nb = *p.count;
+  }
+  // Tile order: b tiles of one a tile are consecutive, then the a tiles, then the splits.
+  const int L = xcd_remap(blockIdx.x, gridDim.x);
+  const int bt = L % p.n_btiles;
+  const int rest = L / p.n_btiles;
+  const int n_atiles = static_cast<int>((p.na + BA - 1) / BA);
+  const int at = rest % n_atiles, split = rest / n_atiles;
+  const int64_t a0 = static_cast<int64_t>(at) * BA, b0 = static_cast<int64_t>(bt) * BB;
+  if (b0 >= nb) return;
+  const int64_t per = ((K + p.splits - 1) / p.splits + 63) / 64 * 64;
+  const int64_t kb = split * per < K ? split * per : K;
+  const int64_t ke = kb + per < K ? kb + per : K;
+  const int nk = static_cast<int>((ke - kb + 63) / 64);
+
+  // Copies. Transposed operand: an instruction covers 512 / columns rows of the stage.
+  constexpr int APR = BA / 8, BPR = TRB ? BB / 8 : 8;  // 16-byte chunks per LDS row
+  uint32_t ca[C::AI], cb[C::BI];                       // column (or row) part of the offset, bytes
+  int ra[C::AI], rb[C::BI];                            // row of the stage (transposed operands)
+#pragma unroll
+  for (int i = 0; i < C::AI; ++i) {
+    const int c = (wave * C::AI + i) * 64 + lane;
+    ra[i] = c / APR;
+    const int64_t col = a0 + 8 * ((c % APR) ^ tr_swz<BA>(ra[i]));
+    ca[i] = static_cast<uint32_t>(2 * (col < p.na ? col : p.na - 8));
+  }
+#pragma unroll
+  for (int i = 0; i < C::BI; ++i) {
+    const int c = (wave * C::BI + i) * 64 + lane;
+    if (TRB) {
+      rb[i] = c / BPR;
+      const int64_t col = b0 + 8 * ((c % BPR) ^ tr_swz<TRB ? BB : 64>(rb[i]));
+      cb[i] = static_cast<uint32_t>(2 * (col < p.ldb ? col : p.ldb - 8));
+    } else {
+      const int r = c / 8;
+      rb[i] = 8 * ((c % 8) ^ row_swz(r));  // first k of the chunk
+      const int64_t gr = r < nb - b0 ? r : nb - b0 - 1;
+      cb[i] = static_cast<uint32_t>(2 * gr * p.ldb);
+    }
+  }
+  const char* const baseA = reinterpret_cast<const char*>(p.A);
+  const char* const baseB =
+      reinterpret_cast<const char*>(p.B) + (TRB ? 0 : static_cast<int64_t>(2) * b0 * p.ldb);
+  const uint32_t lds0 = lds_addr(smem);
+  const uint32_t lda2 = static_cast<uint32_t>(2 * p.lda), ldb2 = static_cast<uint32_t>(2 * p.ldb);
+  // Stage s: rows (or chunks) past the end of the range repeat its last one; what they hold meets
+  // zeros (see tail below).
+  auto copy = [&](int s, int slot) {
+    const int64_t k0 = kb + 64 * static_cast<int64_t>(s);
+    const int left = static_cast<int>(ke - k0 < 64 ? ke - k0 : 64);  // >= 1
+    const uint32_t to = lds0 + slot * C::STAGE;
+    const char* sa = baseA + k0 * lda2;
+    const char* sb = TRB ? baseB + k0 * ldb2 : baseB + 2 * k0;
+#pragma unroll
+    for (int i = 0; i < C::AI; ++i)
+      lds_dma16(sa, ca[i] + static_cast<uint32_t>(ra[i] < left ? ra[i] : left - 1) * lda2,
+                to + (wave * C::AI + i) * 1024);
+#pragma unroll
+    for (int i = 0; i < C::BI; ++i) {
+      const uint32_t off =
+          TRB ? cb[i] + static_cast<uint32_t>(rb[i] < left ? rb[i] : left - 1) * ldb2
+              : cb[i] + 2 * static_cast<uint32_t>(rb[i] < left ? rb[i] : 0);
+      lds_dma16(sb, off, to + C::TILEA + (wave * C::BI + i) * 1024);
+    }
+  };
+
+  f32x16 acc[NRA][NCB];
+#pragma unroll
+  for (int i = 0; i < NRA; ++i)
+#pragma unroll
+    for (int j = 0; j < NCB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  // Fragments of a 16-deep k step: lane l holds column l % 32 of a 32-column block, k values
+  // 8 (l / 32) .. + 7. Transposing read j (of two) takes rows 8 (l / 32) + 4 j + (l % 16) / 4.
+  const int i16 = lane & 15, g16 = (lane >> 4) & 1, half = lane >> 5;
+  auto frag_tr = [&](const char* tile, int row_bytes, int cols64, int block, int ks) {
+    // chunk of the block's 64 bytes: 4 block + 2 g16 + (i16 % 4) / 2, permuted by its row
+    const int k = 16 * ks + 8 * half + (i16 >> 2);
+    const int swz = cols64 ? 4 * ((k >> 1) & 1) : 4 * (k & 3);
+    const int chunk = (4 * block + 2 * g16 + ((i16 & 3) >> 1)) ^ swz;
+    const char* at0 = tile + k * row_bytes + chunk * 16 + (i16 & 1) * 8;
+    return join(lds_read_tr(at0), lds_read_tr(at0 + 4 * row_bytes));
+  };
+  auto stage = [&](int slot, int left) {
+    const char* sa = smem + slot * C::STAGE;
+    const char* sb = sa + C::TILEA;
+    const bool tail = left < 64;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      bf16x8 af[NRA], bf[NCB];
+#pragma unroll
+      for (int i = 0; i < NRA; ++i) af[i] = frag_tr(sa, BA * 2, BA == 64, wa * NRA + i, ks);
+#pragma unroll
+      for (int j = 0; j < NCB; ++j) {
+        if constexpr (TRB) {
+          bf[j] = frag_tr(sb, BB * 2, BB == 64, wb * NCB + j, ks);
+        } else {
+          const int r = (wb * NCB + j) * 32 + (lane & 31);
+          bf[j] = *reinterpret_cast<const bf16x8*>(sb + r * 128 + ((2 * ks + half) ^ row_swz(r)) * 16);
+        }
+        if (tail) bf[j] = keep_first(bf[j], left - 16 * ks - 8 * half);
+      }
+#pragma unroll
+      for (int i = 0; i < NRA; ++i)
+#pragma unroll
+        for (int j = 0; j < NCB; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[i], bf[j], acc[i][j], 0, 0, 0);
+    }
+  };
+
+#pragma unroll
+  for (int j = 0; j < C::S - 1; ++j)
+    if (j < nk) copy(j, j);
+  int slot = 0;
+  for (int kt = 0; kt < nk; ++kt) {
+    // Stages kt + 1 .. kt + S - 2 may still be in flight; near the end all have to be in.
+    if (kt + C::S - 1 <= nk)
+      wait_vmcnt<(C::S - 2) * C::PER>();
+    else
+      wait_vmcnt<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    // Every wave has read stage kt - 1: its slot takes stage kt + S - 1.
+    if (kt + C::S - 1 < nk) copy(kt + C::S - 1, slot == 0 ? C::S - 1 : slot - 1);
+    const int64_t left = ke - kb - 64 * static_cast<int64_t>(kt);
+    stage(slot, left < 64 ? static_cast<int>(left) : 64);
+    slot = slot + 1 == C::S ? 0 : slot + 1;
+  }
+
+  // Lane l holds output row b0 + .. + l % 32 and, in registers 4 g .. 4 g + 3 of block i, columns
+  // 32 i + 8 g + 4 (l / 32) + {0 .. 3}.
+#pragma unroll
+  for (int j = 0; j < NCB; ++j) {
+    const int64_t b = b0 + (wb * NCB + j) * 32 + (lane & 31);
+    if (b >= nb) continue;
+#pragma unroll
+    for (int i = 0; i < NRA; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int64_t a = a0 + (wa * NRA + i) * 32 + 8 * g + 4 * half;
+        if (a >= p.na) continue;  // na % 4 == 0
+        f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        if constexpr (PART) {
+          f32x4* o = reinterpret_cast<f32x4*>(p.part + split * p.part_stride + b * p.na + a);
+          if (p.accumulate) v += *o;
+          *o = v;
+        } else {
+          *reinterpret_cast<bf16x4*>(p.out + b * p.na + a) =
+              bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
+                     static_cast<__bf16>(v[3])};
+        }
+      }
+  }
+}
+
+using Ring128 = RingCfg<128, 128, 2, 2, 2>;
+using Ring64 = RingCfg<128, 64, 2, 2, 3>;
+
+template <class C, bool TRB, bool PART>
+hipError_t launch_ring(Prod p, hipStream_t stream) {
+  const int64_t na = (p.na + C::BA - 1) / C::BA, nb = (p.nb + C::BB - 1) / C::BB;
+  const int64_t n = na * nb * p.splits;
+  if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+  p.n_btiles = static_cast<int>(nb);
+  hipLaunchKernelGGL((prod_ring_kernel<C, TRB, PART>), dim3(static_cast<unsigned>(n)),
+                     dim3(C::kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <bool TRB, bool PART>
+hipError_t launch_prod(const Prod& p, hipStream_t stream) {
+  if (p.nb > 64) return launch_ring<Ring128, TRB, PART>(p, stream);
+  return launch_ring<Ring64, TRB, PART>(p, stream);
+}
+
+// ---------------------------------------------------------------------------------------
+// fp32 GEMM: out(a, b) = sum_k A(k, a) B(k, b) on v_mfma_f32_32x32x2_f32 (fp32 products and sums).
+// 128 x 128 tile, four waves of 128 x 32, 16-deep stages staged through registers. An operand is
+// either [K, n] (TR) or [n, K] row-major; any size and 4-byte alignment.
+
+struct F32Args {
+  const float* A;
+  const float* B;
+  int64_t lda, ldb, na, nb, K;
+  const int32_t* count_b;  // if set: nb
+  const int32_t* count_k;  // if set: K
+  // products
+  float* part;             // [splits, nb_max, na]
+  int64_t part_stride;
+  int accumulate;
+  float* out;              // [nb, na]
+  int splits;
+  int n_btiles;
+  // head
+  const TrainRow* rows;
+  float* lmass;
+  float* tgt;
+  float* grad;
+  int64_t ldg, vbase;
+  int nT;
+};
+
+enum F32Epi : int { kF32Part = 0, kF32Out = 1, kF32Nll = 2, kF32Grad = 3 };
+
+template <bool TRA, bool TRB, int EPI>
+__global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
+  constexpr int BK = 16, LD = 132;
+  __shared__ __attribute__((aligned(16))) float As[2][BK * LD], Bs[2][BK * LD];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int half = lane >> 5;
+  int64_t K = p.count_k ? *p.count_k : p.K;
+  const int64_t nb = p.count_b ? *p.count_b : p.nb;
+  const int n_atiles = static_cast<int>((p.na + 127) / 128);
+  const int bt = blockIdx.x % p.n_btiles, rest = blockIdx.x / p.n_btiles;
+  const int at = rest % n_atiles, split = rest / n_atiles;
+  const int64_t a0 = static_cast<int64_t>(at) * 128, b0 = static_cast<int64_t>(bt) * 128;
+  if (b0 >= nb) return;
+  const int64_t per = ((K + p.splits - 1) / p.splits + BK - 1) / BK * BK;
+  const int64_t kb = split * per < K ? split * per : K;
+  const int64_t ke = kb + per < K ? kb + per : K;
+
+  // 16 x 128 values of an operand, 8 a thread: TR four and four along a row of K, else 8 along K.
+  float ra[8], rb[8];
+  auto load = [&](auto tr, const float* X, int64_t ld, int64_t i0, int64_t n, int64_t k0, float (&r)[8]) {
+    if constexpr (decltype(tr)::value) {
+      const int64_t k = k0 + tid / 16;
+      const int64_t i = i0 + 8 * (tid % 16);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = 0.0f;
+      if (k < ke) {
+        const float* q = X + k * ld + i;
+        if (i + 8 <= n) {
+          const f32x4u u = *reinterpret_cast<const f32x4u*>(q), v = *reinterpret_cast<const f32x4u*>(q + 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            r[j] = u[j];
+            r[4 + j] = v[j];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (i + j < n) r[j] = q[j];
+        }
+      }
+    } else {
+      const int64_t k = k0 + 8 * (tid & 1);
+      const int64_t i = i0 + tid / 2;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = 0.0f;
+      if (i < n) {
+        const float* q = X + i * ld + k;
+        if (k + 8 <= ke) {
+          const f32x4u u = *reinterpret_cast<const f32x4u*>(q), v = *reinterpret_cast<const f32x4u*>(q + 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            r[j] = u[j];
+            r[4 + j] = v[j];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (k + j < ke) r[j] = q[j];
+        }
+      }
+    }
+  };
+  auto store = [&](auto tr, float* S, const float (&r)[8]) {
+    if constexpr (decltype(tr)::value) {
+      float* q = S + (tid / 16) * LD + 8 * (tid % 16);
+      *reinterpret_cast<f32x4*>(q) = f32x4{r[0], r[1], r[2], r[3]};
+      *reinterpret_cast<f32x4*>(q + 4) = f32x4{r[4], r[5], r[6], r[7]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) S[(8 * (tid & 1) + j) * LD + tid / 2] = r[j];
+    }
+  };
+  using TA = std::integral_constant<bool, TRA>;
+  using TB = std::integral_constant<bool, TRB>;
+
+  f32x16 acc[4][1];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][0][r] = 0.0f;
+
+  if (kb < ke) {
+    load(TA{}, p.A, p.lda, a0, p.na, kb, ra);
+    load(TB{}, p.B, p.ldb, b0, nb, kb, rb);
+    store(TA{}, As[0], ra);
+    store(TB{}, Bs[0], rb);
+    __syncthreads();
+    int buf = 0;
+    for (int64_t k0 = kb; k0 < ke; k0 += BK, buf ^= 1) {
+      const bool more = k0 + BK < ke;
+      if (more) {
+        load(TA{}, p.A, p.lda, a0, p.na, k0 + BK, ra);
+        load(TB{}, p.B, p.ldb, b0, nb, k0 + BK, rb);
+      }
+      const float* sa = As[buf] + (lane & 31);
+      const float* sb = Bs[buf] + wave * 32 + (lane & 31);
+#pragma unroll
+      for (int kk = 0; kk < BK; kk += 2) {
+        const float b = sb[(kk + half) * LD];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          acc[i][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(sa[(kk + half) * LD + 32 * i], b, acc[i][0],
+                                                           0, 0, 0);
+      }
+      if (more) {
+        store(TA{}, As[buf ^ 1], ra);
+        store(TB{}, Bs[buf ^ 1], rb);
+      }
+      __syncthreads();
+    }
+  }
+
+  const int64_t b = b0 + wave * 32 + (lane & 31);
+  if constexpr (EPI == kF32Part || EPI == kF32Out) {
+    if (b >= nb) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int64_t a = a0 + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
+        if (a >= p.na) continue;
+        if constexpr (EPI == kF32Part) {
+          float* o = p.part + split * p.part_stride + b * p.na + a;
+          *o = acc[i][0][r] + (p.accumulate ? *o : 0.0f);
+        } else {
+          p.out[b * p.na + a] = acc[i][0][r];
+        }
+      }
+  } else {
+    // a: ids of one vocabulary tile, b: rows (the lane layout of the bf16 head's epilogues).
+    const int lim = static_cast<int>(p.na - a0 < 128 ? p.na - a0 : 128) - 4 * half;
+    if constexpr (EPI == kF32Nll) {
+      float x[64];
+#pragma unroll
+      for (int i = 0; i < 64; ++i)
+        x[i] = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) < lim ? acc[i >> 4][0][i & 15] : -INFINITY;
+      const int64_t o = b < nb ? p.rows[b].token - a0 - 4 * half : -1;
+      if (o >= 0 && o < lim && !(o & 4)) {
+        float t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 64; ++i)
+          t = o == 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) ? x[i] : t;
+        p.tgt[b] = t;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) mx = fmaxf(mx, x[i]);
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      float s = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) s += __expf(x[i] - mx);
+      s += __shfl_xor(s, 32);
+      if (b < nb && half == 0) p.lmass[b * p.nT + a0 / 128] = mx + logf(s);
+    } else {
+      if (b >= nb) return;
+      const TrainRow row = p.rows[b];
+      const int64_t o = row.token - p.vbase - a0 - 4 * half;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          f32x4 y;
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int at0 = 32 * i + 8 * g + q;
+            float u = expf(acc[i][0][4 * g + q] - row.shift);
+            u = o == at0 ? row.at_token : u;
+            y[q] = at0 < lim ? u : 0.0f;
+          }
+          *reinterpret_cast<f32x4*>(p.grad + b * p.ldg + a0 + 32 * i + 8 * g + 4 * half) = y;
+        }
+    }
+  }
+}
+
+template <bool TRA, bool TRB, int EPI>
+hipError_t launch_f32(F32Args p, hipStream_t stream) {
+  const int64_t na = (p.na + 127) / 128, nb = (p.nb + 127) / 128;
+  const int64_t n = na * nb * p.splits;
+  if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+  p.n_btiles = static_cast<int>(nb);
+  hipLaunchKernelGGL((gemm_f32_kernel<TRA, TRB, EPI>), dim3(static_cast<unsigned>(n)), dim3(256), 0,
+                     stream, p);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------
+// dh of every row: the sum of its parts times its scale, 0 for the rows that do not count.
+template <class T>
+__global__ __launch_bounds__(256) void dh_finish_kernel(const NllArgs a, int64_t part_stride) {
+  const int64_t m = blockIdx.x;
+  const int at = a.inv[m / a.R];
+  const int64_t i = static_cast<int64_t>(at) * a.R + m % a.R;
+  const float scale = at >= 0 ? a.rows[i].scale : 0.0f;
+  T* out = static_cast<T*>(a.dh) + m * a.d;
+  if (sizeof(T) == 2) {
+    for (int j = 4 * threadIdx.x; j < a.d; j += 1024) {
+      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (at >= 0) {
+        for (int s = 0; s < a.splits; ++s)
+          v += *reinterpret_cast<const f32x4*>(a.part + s * part_stride + i * a.d + j);
+        v *= scale;
+      }
+      *reinterpret_cast<bf16x4*>(out + j) =
+          bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
+                 static_cast<__bf16>(v[3])};
+    }
+  } else {
+    for (int j = threadIdx.x; j < a.d; j += 256) {
+      float v = 0.0f;
+      if (at >= 0) {
+        for (int s = 0; s < a.splits; ++s) v += a.part[s * part_stride + i * a.d + j];
+        v *= scale;
+      }
+      out[j] = static_cast<T>(v);
+    }
+  }
+}
+
+// The expander's trunk gradient: the product's parts and the residual path's R branch gradients, in
+// fp32, rounded once.
+__global__ __launch_bounds__(256) void expand_dh_finish_kernel(const ExpandBackwardArgs a) {
+  const int64_t p = blockIdx.x;
+  const int d = a.d, R = static_cast<int>(a.R);
+  const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d;
+  for (int j = 4 * threadIdx.x; j < d; j += 1024) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s = 0; s < a.splits; ++s)
+      v += *reinterpret_cast<const f32x4*>(a.part + (static_cast<int64_t>(s) * a.P + p) * d + j);
+    for (int z = 0; z < R; ++z) {
+      const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d + j);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
+    }
+    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.dh) + p * d + j) =
+        bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
+               static_cast<__bf16>(v[3])};
+  }
+}
+
+// dc: the sum over the trunk rows of every branch feature's gradient. A workgroup takes 128 features
+// (16 lanes of 8) with 64 rows side by side.
+__global__ __launch_bounds__(1024) void expand_dc_kernel(const __bf16* __restrict__ dout,
+                                                         __bf16* __restrict__ dc, int64_t P,
+                                                         int64_t n) {
+  __shared__ float part[16][129];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * 128 + 8 * c;
+  float s[8] = {};
+  if (j < n)
+    for (int64_t p = r; p < P; p += 64) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(dout + p * n + j);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s[i] += static_cast<float>(v[i]);
+    }
+  // The four rows of a wave first, then the 16 waves.
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s[i] += __shfl_xor(s[i], 16);
+    s[i] += __shfl_xor(s[i], 32);
+  }
+  if ((threadIdx.x & 63) < 16) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[threadIdx.x >> 6][8 * c + i] = s[i];
+  }
+  __syncthreads();
+  if (threadIdx.x < 128) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += part[i][threadIdx.x];
+    const int64_t o = static_cast<int64_t>(blockIdx.x) * 128 + threadIdx.x;
+    if (o < n) dc[o] = static_cast<__bf16>(t);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_nll(const NllArgs& a, hipStream_t stream) {
+  const int64_t M = a.P * a.R;
+  const int nT = static_cast<int>((a.V + kTile - 1) / kTile);
+  hipError_t e = gather_rows(a, stream);
+  if (e != hipSuccess) return e;
+  if (a.bf16) {
+    HeadTrainArgs h{};
+    h.M = M;
+    h.V = a.V;
+    h.d = a.d;
+    h.h = a.hc;
+    h.w = a.w;
+    h.count = a.count;
+    h.rows = a.rows;
+    h.lmass = a.lmass;
+    h.tgt = a.tgt;
+    e = launch_head_train(h, false, stream);
+  } else {
+    F32Args p{};
+    p.A = static_cast<const float*>(a.w);
+    p.B = static_cast<const float*>(a.hc);
+    p.lda = p.ldb = p.K = a.d;
+    p.na = a.V;
+    p.nb = M;
+    p.count_b = a.count;
+    p.splits = 1;
+    p.rows = a.rows;
+    p.lmass = a.lmass;
+    p.tgt = a.tgt;
+    p.nT = nT;
+    e = launch_f32<false, false, kF32Nll>(p, stream);
+  }
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(nll_finish_kernel, dim3(static_cast<unsigned>((M + 3) / 4)), dim3(256), 0, stream,
+                     a, nT);
+  return hipGetLastError();
+}
+
+hipError_t launch_nll_backward(const NllArgs& a, hipStream_t stream) {
+  const int64_t M = a.P * a.R;
+  hipError_t e = hipSuccess;
+  if (M > 0) e = gather_rows(a, stream);  // without rows dw is 0: a product over no terms
+  if (e != hipSuccess) return e;
+  const int64_t part_stride = M * a.d;
+  for (int64_t v0 = 0; v0 < a.V; v0 += a.piece) {
+    const int64_t n = a.V - v0 < a.piece ? a.V - v0 : a.piece;
+    if (a.bf16) {
+      const __bf16* w = static_cast<const __bf16*>(a.w) + v0 * a.d;
+      if (M > 0) {
+      HeadTrainArgs h{};
+      h.M = M;
+      h.V = n;
+      h.d = a.d;
+      h.h = a.hc;
+      h.w = w;
+      h.count = a.count;
+      h.rows = a.rows;
+      h.grad = a.grad;
+      h.ldg = a.piece;
+      h.vbase = v0;
+      e = launch_head_train(h, true, stream);
+      if (e != hipSuccess) return e;
+      Prod p{};
+      p.A = w;
+      p.lda = p.na = a.d;
+      p.B = static_cast<const __bf16*>(a.grad);
+      p.ldb = a.piece;
+      p.nb = M;
+      p.K = n;
+      p.count = a.count;
+      p.part = a.part;
+      p.part_stride = part_stride;
+      p.accumulate = v0 > 0;
+      p.splits = a.splits;
+      e = launch_prod<false, true>(p, stream);
+      if (e != hipSuccess) return e;
+      }
+      if (a.dw) {
+        Prod q{};
+        q.A = static_cast<const __bf16*>(a.hs);
+        q.lda = q.na = a.d;
+        q.B = static_cast<const __bf16*>(a.grad);
+        q.ldb = a.piece;
+        q.nb = n;
+        q.K = M;
+        q.count = M > 0 ? a.count : nullptr;
+        q.out = static_cast<__bf16*>(a.dw) + v0 * a.d;
+        q.splits = 1;
+        e = launch_prod<true, false>(q, stream);
+      }
+    } else {
+      const float* w = static_cast<const float*>(a.w) + v0 * a.d;
+      if (M > 0) {
+      F32Args p{};
+      p.A = w;
+      p.B = static_cast<const float*>(a.hc);
+      p.lda = p.ldb = p.K = a.d;
+      p.na = n;
+      p.nb = M;
+      p.count_b = a.count;
+      p.splits = 1;
+      p.rows = a.rows;
+      p.grad = static_cast<float*>(a.grad);
+      p.ldg = a.piece;
+      p.vbase = v0;
+      e = launch_f32<false, false, kF32Grad>(p, stream);
+      if (e != hipSuccess) return e;
+      F32Args q{};
+      q.A = w;
+      q.lda = q.na = a.d;
+      q.B = static_cast<const float*>(a.grad);
+      q.ldb = a.piece;
+      q.nb = M;
+      q.K = n;
+      q.count_b = a.count;
+      q.part = a.part;
+      q.part_stride = part_stride;
+      q.accumulate = v0 > 0;
+      q.splits = a.splits;
+      e = launch_f32<true, false, kF32Part>(q, stream);
+      if (e != hipSuccess) return e;
+      }
+      if (a.dw) {
+        F32Args r{};
+        r.A = static_cast<const float*>(a.hs);
+        r.lda = r.na = a.d;
+        r.B = static_cast<const float*>(a.grad);
+        r.ldb = a.piece;
+        r.nb = n;
+        r.K = M;
+        r.count_k = M > 0 ? a.count : nullptr;
+        r.out = static_cast<float*>(a.dw) + v0 * a.d;
+        r.splits = 1;
+        e = launch_f32<true, true, kF32Out>(r, stream);
+      }
+    }
+    if (e != hipSuccess) return e;
+  }
+  if (M == 0) return hipSuccess;
+  const dim3 grid(static_cast<unsigned>(M));
+  if (a.bf16)
+    hipLaunchKernelGGL(dh_finish_kernel<__bf16>, grid, dim3(256), 0, stream, a, part_stride);
+  else
+    hipLaunchKernelGGL(dh_finish_kernel<float>, grid, dim3(256), 0, stream, a, part_stride);
+  return hipGetLastError();
+}
+
+hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t stream) {
+  const int64_t n = a.R * a.d;
+  hipError_t e = hipSuccess;
+  if (a.dh) {
+    Prod p{};
+    p.A = static_cast<const __bf16*>(a.W);
+    p.lda = p.na = a.d;
+    p.B = static_cast<const __bf16*>(a.dout);
+    p.ldb = n;
+    p.nb = a.P;
+    p.K = n;
+    p.part = a.part;
+    p.part_stride = a.P * a.d;
+    p.splits = a.splits;
+    e = launch_prod<false, true>(p, stream);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(expand_dh_finish_kernel, dim3(static_cast<unsigned>(a.P)), dim3(256), 0, stream,
+                       a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.dW) {
+    Prod q{};
+    q.A = static_cast<const __bf16*>(a.h);
+    q.lda = q.na = a.d;
+    q.B = static_cast<const __bf16*>(a.dout);
+    q.ldb = n;
+    q.nb = n;
+    q.K = a.P;
+    q.out = static_cast<__bf16*>(a.dW);
+    q.splits = 1;
+    e = launch_prod<true, false>(q, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (a.dc) {
+    hipLaunchKernelGGL(expand_dc_kernel, dim3(static_cast<unsigned>((n + 127) / 128)), dim3(1024), 0,
+                       stream, static_cast<const __bf16*>(a.dout), static_cast<__bf16*>(a.dc), a.P, n);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace dbl

@@ -20,6 +20,7 @@ DBL_OK, DBL_EINVAL, DBL_ESHAPE, DBL_EDTYPE, DBL_EWORKSPACE, DBL_EHIP = range(6)
 DBL_F32, DBL_BF16 = 0, 1
 (DBL_OP_HEAD, DBL_OP_SAMPLE, DBL_OP_VERIFY, DBL_OP_EXPECTED_LEN, DBL_OP_SAMPLE_GREEDY,
  DBL_OP_VERIFY_GREEDY, DBL_OP_EXPECTED_LEN_GREEDY, DBL_OP_TARGET) = range(8)
+DBL_OP_HEAD_NLL, DBL_OP_HEAD_NLL_BACKWARD, DBL_OP_EXPAND_BACKWARD, DBL_OP_GRAD_NORM = range(16, 20)
 VTILE = 128
 
 
@@ -64,6 +65,12 @@ _SIGS = {
                                                 _P, _P, _P, _P]),
     "dbl_expand_branches": (ctypes.c_int, [Shape, _P, _P, _P, _P, _P]),
     "dbl_prior_head": (ctypes.c_int, [Shape, _P, _P, _P, _P, _P]),
+    "dbl_head_nll": (ctypes.c_int, [Shape, ctypes.c_int, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "dbl_head_nll_backward": (ctypes.c_int, [Shape, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P,
+                                             _P, _SZ, _P]),
+    "dbl_expand_branches_backward": (ctypes.c_int, [Shape, _P, _P, _P, _P, _P, _P, _P, _SZ, _P]),
+    "dbl_grad_norm": (ctypes.c_int, [_I64, _P, _P, _P, _P, _P, _SZ, _P]),
+    "dbl_clip_grads": (ctypes.c_int, [_I64, _P, _P, _P, _P, _P, _F, _P]),
     "dbl_target_logprobs": (ctypes.c_int, [_I64, _I64, _P, _F, _I64, _F, _P, _P, _SZ, _P]),
     "dbl_early_determinism": (ctypes.c_int, [_I64, _I64, _I64, _P, _P, _P, _P, _P]),
     "dbl_stream_read_probe": (ctypes.c_int, [_P, _I64, _P, _I64, _P]),
@@ -417,6 +424,161 @@ def dbl_prior_head(h_anchor, U, e, out=None):
     _check(load().dbl_prior_head(Shape(B, 1, R, d, 1), _ptr(h_anchor), _ptr(U), _ptr(e),
                                  _ptr(out), _stream(dev)))
     return out
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the call's other tensors on {dev}")
+
+
+def _run(fn, dev, *args):
+    """One call with ``dev`` current, as a kernel launch on one of its streams needs."""
+    if dev.index == torch.cuda.current_device():
+        return _check(fn(*args, _stream(dev)))
+    with torch.cuda.device(dev):
+        return _check(fn(*args, _stream(dev)))
+
+
+def _nll_shape(h, w, x):
+    if h.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError("h must be bfloat16 or float32")
+    if h.dim() != 4 or w.dim() != 2:
+        raise ValueError("h must be [B, K, R, d] and w [V, d]")
+    B, K, R, d = h.shape
+    V = w.shape[0]
+    _need(h, "h", h.dtype)
+    _need(w, "w", h.dtype, (V, d))
+    _need(x, "x", torch.int32, (B, K))
+    return Shape(B, K, R, d, V), DBL_BF16 if h.dtype == torch.bfloat16 else DBL_F32
+
+
+def dbl_head_nll(h, w, x, nll=None, lse=None, ws=None):
+    """Negative log-likelihood of tokens x [B, K] int32 under every branch: h [B, K, R, d] and
+    w [V, d] (bf16 or fp32) -> (nll [B, K, R], lse [B, K, R]) fp32. Positions whose token is outside
+    [0, V) do not count: 0 for both."""
+    shape, dt = _nll_shape(h, w, x)
+    dev = h.device
+    rows = (shape.B, shape.K, shape.R)
+    nll = torch.empty(rows, dtype=torch.float32, device=dev) if nll is None else nll
+    lse = nll.new_empty(rows) if lse is None else lse
+    _need(nll, "nll", torch.float32, rows)
+    _need(lse, "lse", torch.float32, rows)
+    ws, nws = _workspace(DBL_OP_HEAD_NLL, shape, dev, ws)
+    _same_device(dev, w=w, x=x, nll=nll, lse=lse, ws=ws)
+    _run(load().dbl_head_nll, dev, shape, dt, _ptr(h), _ptr(w), _ptr(x), _ptr(nll), _ptr(lse),
+         _ptr(ws), nws)
+    return nll, lse
+
+
+def dbl_head_nll_backward(h, w, x, nll, lse, g, want_dw=True, dh=None, dw=None, ws=None):
+    """Gradient through ``dbl_head_nll``: from g = dL/dnll [B, K, R] fp32 and that call's nll and
+    lse, returns (dh [B, K, R, d], dw [V, d]) of h's type, dw None without ``want_dw`` (the head is
+    frozen)."""
+    shape, dt = _nll_shape(h, w, x)
+    dev = h.device
+    rows = (shape.B, shape.K, shape.R)
+    _need(nll, "nll", torch.float32, rows)
+    _need(lse, "lse", torch.float32, rows)
+    _need(g, "g", torch.float32, rows)
+    dh = torch.empty_like(h) if dh is None else dh
+    _need(dh, "dh", h.dtype, h.shape)
+    if want_dw or dw is not None:
+        dw = torch.empty_like(w) if dw is None else dw
+        _need(dw, "dw", h.dtype, w.shape)
+    ws, nws = _workspace(DBL_OP_HEAD_NLL_BACKWARD, shape, dev, ws)
+    _same_device(dev, w=w, x=x, nll=nll, lse=lse, g=g, dh=dh, dw=dw, ws=ws)
+    _run(load().dbl_head_nll_backward, dev, shape, dt, _ptr(h), _ptr(w), _ptr(x), _ptr(nll),
+         _ptr(lse), _ptr(g), _ptr(dh), _ptr(dw), _ptr(ws), nws)
+    return dh, dw
+
+
+def dbl_expand_branches_backward(h, W, dout, want_dh=True, want_dW=True, want_dc=True, dh=None,
+                                 dW=None, dc=None, ws=None):
+    """Gradients through ``dbl_expand_branches``: h [B, K, d], W [R*d, d] and the branch states'
+    gradient dout [B, K, R, d], all bf16 -> (dh [B, K, d], dW [R*d, d], dc [R*d]) bf16, None for
+    what is not wanted."""
+    if h.dim() != 3 or dout.dim() != 4:
+        raise ValueError("h must be [B, K, d] and dout [B, K, R, d]")
+    B, K, d = h.shape
+    R = dout.shape[2]
+    _need(h, "h", torch.bfloat16)
+    _need(W, "W", torch.bfloat16, (R * d, d))
+    _need(dout, "dout", torch.bfloat16, (B, K, R, d))
+    dev = h.device
+    shape = Shape(B, K, R, d, 1)
+    if want_dh or dh is not None:
+        dh = torch.empty_like(h) if dh is None else dh
+        _need(dh, "dh", torch.bfloat16, (B, K, d))
+        ws, nws = _workspace(DBL_OP_EXPAND_BACKWARD, shape, dev, ws)
+    else:
+        ws, nws = None, 0
+    if want_dW or dW is not None:
+        dW = torch.empty_like(W) if dW is None else dW
+        _need(dW, "dW", torch.bfloat16, (R * d, d))
+    if want_dc or dc is not None:
+        dc = W.new_empty(R * d) if dc is None else dc
+        _need(dc, "dc", torch.bfloat16, (R * d,))
+    _same_device(dev, W=W, dout=dout, dh=dh, dW=dW, dc=dc, ws=ws)
+    _run(load().dbl_expand_branches_backward, dev, shape, _ptr(h), _ptr(W), _ptr(dout), _ptr(dh),
+         _ptr(dW), _ptr(dc), _ptr(ws), nws)
+    return dh, dW, dc
+
+
+_GRAD_TYPES = {torch.float32: DBL_F32, torch.bfloat16: DBL_BF16}
+
+
+def _tensors(ts, name, dev):
+    """Addresses of a list of gradients (bf16 or fp32, contiguous, on ``dev``)."""
+    for t in ts:
+        if not (t.dtype in _GRAD_TYPES and t.is_contiguous() and t.device == dev):
+            if t.dtype not in _GRAD_TYPES:
+                raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+            raise ValueError(f"{name} must be on one GPU, got {t.device} beside {dev}")
+    return (_P * len(ts))(*[t.data_ptr() for t in ts])
+
+
+def _grads(grads):
+    grads = list(grads)
+    dev = grads[0].device if grads else None
+    if dev is not None and dev.type != "cuda":
+        raise ValueError("grads must be GPU tensors")
+    n = len(grads)
+    return (grads, dev, _tensors(grads, "grads", dev), (_I64 * n)(*[t.numel() for t in grads]),
+            (ctypes.c_int32 * n)(*[_GRAD_TYPES[t.dtype] for t in grads]))
+
+
+def dbl_grad_norm(grads, norm=None, ws=None):
+    """Euclidean norm of a list of gradients (bf16 or fp32, contiguous, one GPU) taken together: a
+    0-dimensional fp32 tensor on their GPU (``norm`` if given)."""
+    grads, dev, ptrs, numel, dt = _grads(grads)
+    if dev is None:
+        raise ValueError("grads is empty")
+    norm = torch.empty((), dtype=torch.float32, device=dev) if norm is None else norm
+    _need(norm, "norm", torch.float32, ())
+    ws, nws = _workspace(DBL_OP_GRAD_NORM, Shape(len(grads), 1, 1, 1, 1), dev, ws)
+    _same_device(dev, norm=norm, ws=ws)
+    _run(load().dbl_grad_norm, dev, len(grads), ptrs, numel, dt, _ptr(norm), _ptr(ws), nws)
+    return norm
+
+
+def dbl_clip_grads(grads, norm, max_norm, out=None):
+    """Gradients times min(1, max_norm / (norm + 1e-6)): in place, or into the tensors ``out`` (same
+    types and sizes). ``norm`` is a 0-dimensional fp32 GPU tensor. Returns the list of outputs."""
+    grads, dev, ptrs, numel, dt = _grads(grads)
+    if dev is None:
+        return []
+    _need(norm, "norm", torch.float32, ())
+    _same_device(dev, norm=norm)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads) or any(o.dtype != t.dtype or o.shape != t.shape
+                                      for o, t in zip(outs, grads)):
+        raise ValueError("out must hold a tensor of the same type and shape for every gradient")
+    to = None if out is None else _tensors(outs, "out", dev)
+    _run(load().dbl_clip_grads, dev, len(grads), ptrs, to, numel, dt, _ptr(norm), float(max_norm))
+    return outs
 
 
 def dbl_target_logprobs(logits, temperature=1.0, top_k=0, top_p=1.0, out=None, ws=None,
