@@ -57,11 +57,24 @@ __device__ __forceinline__ void add_square(double& s, float x) {
   s = fma(y, y, s);
 }
 
-__global__ __launch_bounds__(256) void norm_part_kernel(const NormSet s, int chunks,
+// The tensor of chunk c: the last one whose first chunk is not past it (by halves: walking the list, a
+// scalar load a tensor, took most of the time of many small tensors).
+template <class Set>
+__device__ __forceinline__ int tensor_of(const Set& s, int count, int c) {
+  int lo = 0, hi = count;  // first[lo] <= c < first[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (s.first[mid] <= c) lo = mid;
+    else hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(256) void norm_part_kernel(const NormSet s, int count, int chunks,
                                                         double* __restrict__ part) {
   const int tid = threadIdx.x;
   double acc[4] = {0.0, 0.0, 0.0, 0.0};
-  int t = 0;
+  int t = tensor_of(s, count, blockIdx.x);
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
     while (c >= s.first[t + 1]) ++t;
     const int64_t at = (c - s.first[t]) * kChunk;
@@ -101,13 +114,13 @@ __global__ __launch_bounds__(256) void norm_finish_kernel(const double* __restri
 
 // g * scale in fp32, rounded once to the tensor's type. `same`: whether the outputs are the gradients
 // themselves, which a scale of 1 leaves alone.
-__global__ __launch_bounds__(256) void clip_kernel(const ClipSet s, int chunks, int same,
+__global__ __launch_bounds__(256) void clip_kernel(const ClipSet s, int count, int chunks, int same,
                                                    const float* __restrict__ norm, float max_norm) {
   const float ratio = max_norm / (*norm + 1e-6f);
   const float scale = ratio > 1.0f ? 1.0f : ratio;  // NaN stays
   if (same && scale == 1.0f) return;
   const int tid = threadIdx.x;
-  int t = 0;
+  int t = tensor_of(s, count, blockIdx.x);
   for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
     while (c >= s.first[t + 1]) ++t;
     const int64_t at = (c - s.first[t]) * kChunk;
@@ -143,9 +156,9 @@ __global__ __launch_bounds__(256) void clip_kernel(const ClipSet s, int chunks, 
 
 // The next tensors (at most `most`, empty ones left out) into a launch's set; returns the chunks.
 template <class Set, class Extra>
-int fill(Set& s, int most, const GradTensor* t, int64_t n, int64_t& next, Extra extra) {
+int fill(Set& s, int most, const GradTensor* t, int64_t n, int64_t& next, int& k, Extra extra) {
   int64_t chunks = 0;
-  int k = 0;
+  k = 0;
   for (; next < n && k < most; ++next) {
     if (t[next].n == 0) continue;
     s.g[k] = t[next].g;
@@ -170,10 +183,12 @@ hipError_t launch_grad_norm(const GradTensor* t, int64_t n, double* part, float*
   int64_t next = 0, parts = 0;
   while (next < n) {
     NormSet s;
-    const int chunks = fill(s, kNormSet, t, n, next, [](int, const GradTensor&) {});
+    int count;
+    const int chunks = fill(s, kNormSet, t, n, next, count, [](int, const GradTensor&) {});
     if (chunks == 0) continue;
     const int blocks = blocks_for(chunks);
-    hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(256), 0, stream, s, chunks, part + parts);
+    hipLaunchKernelGGL(norm_part_kernel, dim3(blocks), dim3(256), 0, stream, s, count, chunks,
+                       part + parts);
     parts += blocks;
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -189,10 +204,12 @@ hipError_t launch_clip_grads(const GradTensor* t, int64_t n, const float* norm, 
   for (int64_t i = 0; i < n; ++i) same = same && (t[i].out == t[i].g || t[i].n == 0);
   while (next < n) {
     ClipSet s;
+    int count;
     const int chunks =
-        fill(s, kClipSet, t, n, next, [&](int k, const GradTensor& g) { s.out[k] = g.out; });
+        fill(s, kClipSet, t, n, next, count,
+             [&](int k, const GradTensor& g) { s.out[k] = g.out; });
     if (chunks == 0) continue;
-    hipLaunchKernelGGL(clip_kernel, dim3(blocks_for(chunks)), dim3(256), 0, stream, s, chunks,
+    hipLaunchKernelGGL(clip_kernel, dim3(blocks_for(chunks)), dim3(256), 0, stream, s, count, chunks,
                        same ? 1 : 0, norm, max_norm);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

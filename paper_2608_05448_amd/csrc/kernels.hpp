@@ -231,15 +231,38 @@ inline int64_t nll_piece(int64_t M, int64_t V, int elem) {
   return (each + 4095) / 4096 * 4096;
 }
 
-// How many parts the sum over K of an [nb, na] product is split into, so that `tile` x `tile` output
-// tiles times parts fill the chip (a part has 256 terms at least).
+// The kernel of a bf16 product [nb, na] over K terms (both: both operands lie across the sum): 256 x 256
+// tiles, one workgroup to a CU; 256-column tiles of up to 128 rows, one to a CU; smaller tiles.
+enum ProdKind : int { kProdPp = 0, kProdFew = 1, kProdSmall = 2 };
+inline ProdKind prod_kind(bool both, int64_t na, int64_t nb, int64_t K) {
+  if (na > 128 && nb > 128 && K >= 512) return kProdPp;
+  return !both && na > 128 && nb <= 128 ? kProdFew : kProdSmall;
+}
+
+// How many parts the sum over K of an [nb, na] product is split into (one operand across the sum).
+// 256 x 256 tiles: the split with the least time for whole rounds of 256 workgroups, at 1.7 us a 64-deep
+// stage and 20 us a tile for its stores and their sum. Others: as many as one round of workgroups holds,
+// of 256 terms at least.
 inline int grad_splits(int64_t na, int64_t nb, int64_t K) {
-  const int64_t tiles = ((na + 127) / 128) * ((nb + 127) / 128);
-  if (tiles == 0) return 1;
-  int64_t s = (512 + tiles - 1) / tiles;
+  if (na <= 0 || nb <= 0 || K <= 0) return 1;
+  const ProdKind kind = prod_kind(false, na, nb, K);
+  if (kind == kProdPp) {
+    const int64_t tiles = ((na + 255) / 256) * ((nb + 255) / 256), stages = (K + 63) / 64;
+    int best = 1;
+    int64_t least = 0;
+    for (int s = 1; s <= 64 && stages / s >= 4; ++s) {
+      const int64_t t = (tiles * s + 255) / 256 * ((stages + s - 1) / s * 17 + 200);
+      if (s == 1 || t < least) {
+        least = t;
+        best = s;
+      }
+    }
+    return best;
+  }
+  const int64_t s = kind == kProdFew ? 256 / ((na + 255) / 256)
+                                     : 512 / (((na + 127) / 128) * ((nb + 127) / 128));
   const int64_t most = (K + 255) / 256;
-  s = s < most ? s : most;
-  return static_cast<int>(s < 1 ? 1 : s);
+  return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
 }
 
 constexpr int64_t kMaxTrainRows = 0x7fffffff;

@@ -74,14 +74,13 @@ __global__ __launch_bounds__(1024) void count_positions_kernel(const int32_t* __
   if (threadIdx.x == 0) *count = before * R;
 }
 
-// One workgroup per position: its place among the positions that count, its R rows of h copied there
-// (and, for dw, times their scale), and what the head's kernels need of each row.
+// One workgroup per row: its position's place among those that count, its states copied there (and, for
+// dw, times their scale), and what the head's kernels need of it.
 template <class T>
 __global__ __launch_bounds__(256) void gather_rows_kernel(const NllArgs a, int counted) {
   __shared__ int part[4];
-  __shared__ float scale[kMaxR];
   const int64_t p = blockIdx.x;
-  const int R = static_cast<int>(a.R), d = a.d;
+  const int R = static_cast<int>(a.R), d = a.d, r = blockIdx.y;
   const int32_t token = a.x[p];
   const bool mine = counts(token, a.V);
   int at;
@@ -94,57 +93,50 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const NllArgs a, int c
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = c;
     __syncthreads();
     at = part[0] + part[1] + part[2] + part[3];
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == 0 && r == 0) {
       a.inv[p] = mine ? at : -1;
       if (p == a.P - 1) *a.count = (at + (mine ? 1 : 0)) * R;
     }
   }
   if (!mine) return;
-  const int64_t to = static_cast<int64_t>(at) * R;
-  if (static_cast<int>(threadIdx.x) < R) {
-    const int r = threadIdx.x;
-    TrainRow row{0.0f, 0.0f, 0.0f, token};
-    if (a.g) {
-      const float lse = a.lse[p * R + r], g = a.g[p * R + r];
-      const float q = -expm1f(-fmaxf(a.nll[p * R + r], 0.0f));
-      if (sizeof(T) == 2) {
-        const float qc = fmaxf(q, 0x1p-24f);
-        row.shift = (lse + logf(qc)) * kLog2e;
-        row.at_token = -q / qc;
-        row.scale = g * qc;
-      } else {
-        row.shift = lse;
-        row.at_token = -q;
-        row.scale = g;
-      }
+  const int64_t from = p * R + r, to = static_cast<int64_t>(at) * R + r;
+  TrainRow row{0.0f, 0.0f, 0.0f, token};
+  if (a.g) {
+    const float lse = a.lse[from], g = a.g[from];
+    const float q = -expm1f(-fmaxf(a.nll[from], 0.0f));
+    if (sizeof(T) == 2) {
+      const float qc = fmaxf(q, 0x1p-24f);
+      row.shift = (lse + logf(qc)) * kLog2e;
+      row.at_token = -q / qc;
+      row.scale = g * qc;
+    } else {
+      row.shift = lse;
+      row.at_token = -q;
+      row.scale = g;
     }
-    a.rows[to + r] = row;
-    scale[r] = row.scale;
   }
-  __syncthreads();
-  const T* src = static_cast<const T*>(a.h) + p * R * d;
+  if (threadIdx.x == 0) a.rows[to] = row;
+  const T* src = static_cast<const T*>(a.h) + from * d;
   T* dst = static_cast<T*>(a.hc) + to * d;
   T* dss = a.hs ? static_cast<T*>(a.hs) + to * d : nullptr;
   if (sizeof(T) == 2) {  // d % 8 == 0
-    for (int r = 0; r < R; ++r)
-      for (int j = 8 * threadIdx.x; j < d; j += 2048) {
-        const bf16x8 v = *reinterpret_cast<const bf16x8*>(src + static_cast<int64_t>(r) * d + j);
-        *reinterpret_cast<bf16x8*>(dst + static_cast<int64_t>(r) * d + j) = v;
-        if (dss) {
-          bf16x8 y;
+#pragma unroll 2
+    for (int j = 8 * threadIdx.x; j < d; j += 2048) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(src + j);
+      *reinterpret_cast<bf16x8*>(dst + j) = v;
+      if (dss) {
+        bf16x8 y;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = static_cast<__bf16>(static_cast<float>(v[i]) * scale[r]);
-          *reinterpret_cast<bf16x8*>(dss + static_cast<int64_t>(r) * d + j) = y;
-        }
+        for (int i = 0; i < 8; ++i) y[i] = static_cast<__bf16>(static_cast<float>(v[i]) * row.scale);
+        *reinterpret_cast<bf16x8*>(dss + j) = y;
       }
+    }
   } else {
-    for (int r = 0; r < R; ++r)
-      for (int j = threadIdx.x; j < d; j += 256) {
-        const int64_t o = static_cast<int64_t>(r) * d + j;
-        const T v = src[o];
-        dst[o] = v;
-        if (dss) dss[o] = static_cast<T>(static_cast<float>(v) * scale[r]);
-      }
+    for (int j = threadIdx.x; j < d; j += 256) {
+      const T v = src[j];
+      dst[j] = v;
+      if (dss) dss[j] = static_cast<T>(static_cast<float>(v) * row.scale);
+    }
   }
 }
 
@@ -153,7 +145,7 @@ hipError_t gather_rows(const NllArgs& a, hipStream_t stream) {
   if (counted)
     hipLaunchKernelGGL(count_positions_kernel, dim3(1), dim3(1024), 0, stream, a.x, a.P,
                        static_cast<int>(a.R), a.V, a.inv, a.count);
-  const dim3 grid(static_cast<unsigned>(a.P));
+  const dim3 grid(static_cast<unsigned>(a.P), static_cast<unsigned>(a.R));
   if (a.bf16)
     hipLaunchKernelGGL(gather_rows_kernel<__bf16>, grid, dim3(256), 0, stream, a, counted);
   else
@@ -161,8 +153,11 @@ hipError_t gather_rows(const NllArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-// lse and nll of every row from the tile log-masses; 0 for the rows that do not count. One wave a row.
+// lse and nll of every row from the tile log-masses; 0 for the rows that do not count. One wave a row,
+// 32 masses a lane at a time (V up to 262,144 in one pass): all loads in flight, then their maximum and
+// their sum of exponentials, joined to the running ones.
 __global__ __launch_bounds__(256) void nll_finish_kernel(const NllArgs a, int nT) {
+  constexpr int kRegs = 32;
   const int64_t m = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (m >= a.P * a.R) return;
@@ -172,17 +167,28 @@ __global__ __launch_bounds__(256) void nll_finish_kernel(const NllArgs a, int nT
     const int64_t i = static_cast<int64_t>(at) * a.R + m % a.R;
     const float* row = a.lmass + i * nT;
     float mx = -INFINITY, s = 0.0f;
-    for (int t = lane; t < nT; t += 64) {  // running maximum and sum
-      const float v = row[t], top = fmaxf(mx, v);
-      s = top > -INFINITY ? s * expf(mx - top) + expf(v - top) : 0.0f;
+    for (int t0 = 0; t0 < nT; t0 += 64 * kRegs) {
+      float v[kRegs], top = mx;
+#pragma unroll
+      for (int k = 0; k < kRegs; ++k) {
+        const int t = t0 + lane + 64 * k;
+        v[k] = t < nT ? row[t] : -INFINITY;
+      }
+#pragma unroll
+      for (int k = 0; k < kRegs; ++k) top = fmaxf(top, v[k]);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+      float add = 0.0f;
+      if (top > -INFINITY) {
+        s *= expf(mx - top);
+#pragma unroll
+        for (int k = 0; k < kRegs; ++k) add += expf(v[k] - top);
+      }
+      s += add;
       mx = top;
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      const float omx = __shfl_xor(mx, o), os = __shfl_xor(s, o), top = fmaxf(mx, omx);
-      s = top > -INFINITY ? s * expf(mx - top) + os * expf(omx - top) : 0.0f;
-      mx = top;
-    }
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
     lse = mx + logf(s);
     nll = lse - a.tgt[i];
   }
@@ -216,9 +222,15 @@ __device__ __forceinline__ uint32_t lds_addr(const char* p) {
 // One global_load_lds_dwordx4 (lane i copies 16 bytes from sbase + voff to LDS byte m0 + 16 i), issued
 // through inline asm so that the compiler does not drain every outstanding copy before each LDS read;
 // completion is tracked with wait_vmcnt. The wait states cover a VALU write of the scalar base.
+// NT: non-temporal, for an operand that the launch reads once.
+template <bool NT = false>
 __device__ __forceinline__ void lds_dma16(const char* sbase, uint32_t voff, uint32_t m0v) {
-  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(m0v)
-               : "memory");
+  if constexpr (NT)
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(voff), "s"(sbase), "{m0}"(m0v)
+                 : "memory");
+  else
+    asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(m0v)
+                 : "memory");
 }
 
 template <int N>
@@ -265,19 +277,90 @@ __device__ __forceinline__ int tr_swz(int k) {
 // LDS layout of an operand held along K: 128-byte rows, chunk c of row r at chunk c ^ ((r / 2) % 8).
 __device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
 
-// Ring kernel: BA x BB output tile, WA x WB waves, 64-deep stages copied global -> LDS into an S-slot
+// Stores a wave's block of outputs, 32 rows x 32 NRA columns at a time through LDS so that a store
+// instruction writes whole row segments (the register layout would write 8 or 16 bytes of 32 rows): lane
+// l holds row l % 32 and, in registers 4 g .. 4 g + 3 of block i, columns 32 i + 8 g + 4 (l / 32) + {0 .. 3}.
+// xp: 32 rows of 32 NRA values of LDS that no other wave touches. Chunks of a row are permuted by the row.
+template <int NRA, int NCB, bool PART>
+__device__ __forceinline__ void store_block(f32x16 (&acc)[NRA][NCB], const Prod& p, int64_t nb,
+                                            int64_t b0, int64_t a0, int split, int lane, char* xp) {
+  constexpr int COLS = 32 * NRA, ROWB = COLS * (PART ? 4 : 2), CH = ROWB / 16;  // 16-byte chunks a row
+  constexpr int RPI = 64 / CH;                                                // rows per instruction
+  static_assert(CH >= 4 && CH <= 64 && (CH & (CH - 1)) == 0, "whole rows per instruction");
+  const int lr = lane & 31, half = lane >> 5;
+  constexpr int MASK = CH < 16 ? CH - 1 : 15;
+#pragma unroll
+  for (int j = 0; j < NCB; ++j) {
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NRA; ++i)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const f32x16& v = acc[i][j];
+        if constexpr (PART)
+          *reinterpret_cast<f32x4*>(xp + lr * ROWB + ((8 * i + 2 * g + half) ^ (lr & MASK)) * 16) =
+              f32x4{v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]};
+        else
+          *reinterpret_cast<bf16x4*>(xp + lr * ROWB + ((4 * i + g) ^ (lr & MASK)) * 16 + half * 8) =
+              bf16x4{static_cast<__bf16>(v[4 * g]), static_cast<__bf16>(v[4 * g + 1]),
+                     static_cast<__bf16>(v[4 * g + 2]), static_cast<__bf16>(v[4 * g + 3])};
+      }
+    // Wave-private LDS region: the writes above precede these reads in the wave's LDS queue.
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+    for (int r0 = 0; r0 < 32; r0 += RPI) {
+      const int r = r0 + lane / CH, c = lane % CH;
+      const int64_t b = b0 + 32 * j + r, a = a0 + c * (PART ? 4 : 8);
+      const char* at = xp + r * ROWB + (c ^ (r & MASK)) * 16;
+      if (b < nb && a < p.na) {  // na % 8 == 0
+        if constexpr (PART) {
+          f32x4 v = *reinterpret_cast<const f32x4*>(at);
+          f32x4* o = reinterpret_cast<f32x4*>(p.part + split * p.part_stride + b * p.na + a);
+          if (p.accumulate) v += *o;
+          *o = v;
+        } else {
+          *reinterpret_cast<u32x4*>(p.out + b * p.na + a) = *reinterpret_cast<const u32x4*>(at);
+        }
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+}
+
+// Tile order: groups of kGroupB b tiles; a group sweeps every a tile before the next group starts, its b
+// tiles consecutive for one a tile, so that the 32 workgroups of an XCD share 8 a and 4 b tiles. The
+// splits of the sum come one after the other.
+constexpr int kGroupB = 4;
+__device__ __forceinline__ void prod_tile(int L, int n_atiles, int n_btiles, int* at, int* bt, int* split) {
+  const int n = n_atiles * n_btiles;
+  *split = L / n;
+  L -= *split * n;
+  const int full = n_btiles / kGroupB * kGroupB * n_atiles;
+  const int g = L < full ? kGroupB : n_btiles % kGroupB;
+  const int base = L < full ? L / (kGroupB * n_atiles) * kGroupB : n_btiles - g;
+  const int rem = L < full ? L % (kGroupB * n_atiles) : L - full;
+  // In scalar registers: the copies' base addresses are made of these.
+  *split = __builtin_amdgcn_readfirstlane(*split);
+  *at = __builtin_amdgcn_readfirstlane(rem / g);
+  *bt = __builtin_amdgcn_readfirstlane(base + rem % g);
+}
+
+// Ring kernel: BA x BB output tile, WA x WB waves, BK-deep stages copied global -> LDS into an S-slot
 // ring S - 1 stages ahead, one barrier per stage.
-template <int BA_, int BB_, int WA_, int WB_, int S_>
+template <int BA_, int BB_, int WA_, int WB_, int S_, int BK_ = 64, bool NT_ = false>
 struct RingCfg {
-  static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = WB_, S = S_;
+  static constexpr int BA = BA_, BB = BB_, WA = WA_, WB = WB_, S = S_, BK = BK_;
+  static constexpr bool NT = NT_;
   static constexpr int NW = WA * WB, kThreads = 64 * NW;
   static constexpr int NRA = BA / WA / 32, NCB = BB / WB / 32;
-  static constexpr int TILEA = BA * 128, TILEB = BB * 128, STAGE = TILEA + TILEB;
+  static constexpr int TILEA = BA * BK * 2, TILEB = BB * BK * 2, STAGE = TILEA + TILEB;
   static constexpr int AI = TILEA / 1024 / NW, BI = TILEB / 1024 / NW;  // copies per wave and stage
   static constexpr int PER = AI + BI;
   static constexpr int kLds = S * STAGE;
   static constexpr int kWgPerCu = 160 * 1024 / kLds;
-  static constexpr int kWavesPerEu = kWgPerCu * NW < 8 ? 1 : kWgPerCu * NW < 16 ? 2 : 4;
+  static constexpr int kWavesPerEu = kWgPerCu * NW / 4 < 1 ? 1 : kWgPerCu * NW / 4;
   static_assert(TILEA % (1024 * NW) == 0 && TILEB % (1024 * NW) == 0, "whole copies");
   static_assert(NRA >= 1 && NCB >= 1 && BA % (32 * WA) == 0 && BB % (32 * WB) == 0, "tiling");
   static_assert((S - 1) * PER <= 63 && kLds <= 160 * 1024, "ring");
@@ -285,7 +368,8 @@ struct RingCfg {
 
 template <class C, bool TRB, bool PART>
 __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(const Prod p) {
-  constexpr int BA = C::BA, BB = C::BB, NRA = C::NRA, NCB = C::NCB;
+  constexpr int BA = C::BA, BB = C::BB, NRA = C::NRA, NCB = C::NCB, BK = C::BK;
+  static_assert(TRB || BK == 64, "an operand held along K has 128-byte LDS rows");
   __shared__ __attribute__((aligned(1024))) char smem[C::kLds];
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -297,18 +381,16 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
     if (TRB) K = *p.count;
     else nb = *p.count;
   }
-  // Tile order: b tiles of one a tile are consecutive, then the a tiles, then the splits.
-  const int L = xcd_remap(blockIdx.x, gridDim.x);
-  const int bt = L % p.n_btiles;
-  const int rest = L / p.n_btiles;
-  const int n_atiles = static_cast<int>((p.na + BA - 1) / BA);
-  const int at = rest % n_atiles, split = rest / n_atiles;
+  int at, bt, split;
+  prod_tile(xcd_remap(blockIdx.x, gridDim.x), static_cast<int>((p.na + BA - 1) / BA), p.n_btiles, &at,
+            &bt, &split);
   const int64_t a0 = static_cast<int64_t>(at) * BA, b0 = static_cast<int64_t>(bt) * BB;
   if (b0 >= nb) return;
-  const int64_t per = ((K + p.splits - 1) / p.splits + 63) / 64 * 64;
-  const int64_t kb = split * per < K ? split * per : K;
-  const int64_t ke = kb + per < K ? kb + per : K;
-  const int nk = static_cast<int>((ke - kb + 63) / 64);
+  // Stages are dealt to the splits in turn, so that all of them read one front that moves through the
+  // operands (60 rows, d = 2560, K = 151,936: 136 us; with a range of its own for each split 144).
+  const int64_t stages = (K + BK - 1) / BK;
+  const int nk = static_cast<int>(stages > split ? (stages - split + p.splits - 1) / p.splits : 0);
+  const int64_t kb = static_cast<int64_t>(split) * BK, step = static_cast<int64_t>(p.splits) * BK;
 
   // Copies. Transposed operand: an instruction covers 512 / columns rows of the stage.
   constexpr int APR = BA / 8, BPR = TRB ? BB / 8 : 8;  // 16-byte chunks per LDS row
@@ -343,14 +425,14 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
   // Stage s: rows (or chunks) past the end of the range repeat its last one; what they hold meets
   // zeros (see tail below).
   auto copy = [&](int s, int slot) {
-    const int64_t k0 = kb + 64 * static_cast<int64_t>(s);
-    const int left = static_cast<int>(ke - k0 < 64 ? ke - k0 : 64);  // >= 1
+    const int64_t k0 = kb + step * static_cast<int64_t>(s);
+    const int left = static_cast<int>(K - k0 < BK ? K - k0 : BK);  // >= 1
     const uint32_t to = lds0 + slot * C::STAGE;
     const char* sa = baseA + k0 * lda2;
     const char* sb = TRB ? baseB + k0 * ldb2 : baseB + 2 * k0;
 #pragma unroll
     for (int i = 0; i < C::AI; ++i)
-      lds_dma16(sa, ca[i] + static_cast<uint32_t>(ra[i] < left ? ra[i] : left - 1) * lda2,
+      lds_dma16<C::NT>(sa, ca[i] + static_cast<uint32_t>(ra[i] < left ? ra[i] : left - 1) * lda2,
                 to + (wave * C::AI + i) * 1024);
 #pragma unroll
     for (int i = 0; i < C::BI; ++i) {
@@ -383,9 +465,9 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
   auto stage = [&](int slot, int left) {
     const char* sa = smem + slot * C::STAGE;
     const char* sb = sa + C::TILEA;
-    const bool tail = left < 64;
+    const bool tail = left < BK;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
+    for (int ks = 0; ks < BK / 16; ++ks) {
       bf16x8 af[NRA], bf[NCB];
 #pragma unroll
       for (int i = 0; i < NRA; ++i) af[i] = frag_tr(sa, BA * 2, BA == 64, wa * NRA + i, ks);
@@ -422,39 +504,240 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
     asm volatile("" ::: "memory");
     // Every wave has read stage kt - 1: its slot takes stage kt + S - 1.
     if (kt + C::S - 1 < nk) copy(kt + C::S - 1, slot == 0 ? C::S - 1 : slot - 1);
-    const int64_t left = ke - kb - 64 * static_cast<int64_t>(kt);
-    stage(slot, left < 64 ? static_cast<int>(left) : 64);
+    const int64_t left = K - kb - step * static_cast<int64_t>(kt);
+    stage(slot, left < BK ? static_cast<int>(left) : BK);
     slot = slot + 1 == C::S ? 0 : slot + 1;
   }
 
-  // Lane l holds output row b0 + .. + l % 32 and, in registers 4 g .. 4 g + 3 of block i, columns
-  // 32 i + 8 g + 4 (l / 32) + {0 .. 3}.
-#pragma unroll
-  for (int j = 0; j < NCB; ++j) {
-    const int64_t b = b0 + (wb * NCB + j) * 32 + (lane & 31);
-    if (b >= nb) continue;
-#pragma unroll
-    for (int i = 0; i < NRA; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int64_t a = a0 + (wa * NRA + i) * 32 + 8 * g + 4 * half;
-        if (a >= p.na) continue;  // na % 4 == 0
-        f32x4 v = {acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
-        if constexpr (PART) {
-          f32x4* o = reinterpret_cast<f32x4*>(p.part + split * p.part_stride + b * p.na + a);
-          if (p.accumulate) v += *o;
-          *o = v;
-        } else {
-          *reinterpret_cast<bf16x4*>(p.out + b * p.na + a) =
-              bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
-                     static_cast<__bf16>(v[3])};
-        }
-      }
-  }
+  // The ring is free once every wave has left its last stage (every copy has landed).
+  __syncthreads();
+  constexpr int XP = 32 * 32 * NRA * (PART ? 4 : 2);
+  static_assert(C::NW * XP <= C::kLds, "LDS for the stores");
+  store_block<NRA, NCB, PART>(acc, p, nb, b0 + wb * NCB * 32, a0 + wa * NRA * 32, split, lane,
+                              smem + wave * XP);
 }
 
-using Ring128 = RingCfg<128, 128, 2, 2, 2>;
-using Ring64 = RingCfg<128, 64, 2, 2, 3>;
+// Ping-pong kernel: 256 x 256 output tile, 64-deep stages, 8 waves of 128 a x 64 b in two groups of four
+// that take turns between workgroup barriers: one group issues MFMAs (16 a turn, 32 of a stage's 64 k)
+// while the other reads its next fragments from LDS and issues global -> LDS copies (4 a wave and turn).
+// The dispatcher places waves w and w + 4 on the same SIMD, so that each SIMD's matrix pipe is fed by
+// one wave or the other. LDS: three slots of A stages and two of B stages (160 KB). Copies: even turn 2 s
+// the B rows of stage s + 1, odd turn 2 s + 1 the A rows of stage s + 2.
+constexpr int kPpTile = 32768;  // bytes of an operand's stage
+__device__ __forceinline__ void pp_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+template <bool TRB, bool PART>
+__global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
+  constexpr int NRA = 4, NCB = 2, TILE = kPpTile, BOFF = 3 * TILE;
+  __shared__ __attribute__((aligned(1024))) char smem[5 * TILE];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int grp = wave >> 2;  // group 0 computes first in every pair of turns
+  const int wa = wave & 1;    // half of the 256 a
+  const int wb = wave >> 1;   // quarter of the 256 b
+
+  int64_t K = p.K, nb = p.nb;
+  if (p.count) {
+    if (TRB) K = *p.count;
+    else nb = *p.count;
+  }
+  int at, bt, split;
+  prod_tile(xcd_remap(blockIdx.x, gridDim.x), static_cast<int>((p.na + 255) / 256), p.n_btiles, &at,
+            &bt, &split);
+  const int64_t a0 = static_cast<int64_t>(at) * 256, b0 = static_cast<int64_t>(bt) * 256;
+  if (b0 >= nb) return;
+  const int64_t per = ((K + p.splits - 1) / p.splits + 63) / 64 * 64;
+  const int64_t kb = split * per < K ? split * per : K;
+  const int64_t ke = kb + per < K ? kb + per : K;
+  const int nk = static_cast<int>((ke - kb + 63) / 64);
+
+  // Copy i of a wave: rows 2 (4 wave + i) + lane / 32 of a transposed operand's stage (512 bytes each),
+  // rows 8 (4 wave + i) + lane / 8 of an operand held along K (128 bytes each). The lane's place in the
+  // LDS row fetches the chunk that is permuted there. Columns past the operand's end repeat its last
+  // chunk (they reach outputs past the end only).
+  const uint32_t lda2 = static_cast<uint32_t>(2 * p.lda), ldb2 = static_cast<uint32_t>(2 * p.ldb);
+  uint32_t offA[4], offB[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 2 * (4 * wave + i) + (lane >> 5);
+    const int c = 8 * ((lane & 31) ^ tr_swz<256>(r));
+    const int64_t ca = a0 + c < p.na ? a0 + c : p.na - 8;
+    offA[i] = static_cast<uint32_t>(2 * ca) + r * lda2;
+    if (TRB) {
+      const int64_t cb = b0 + c < p.ldb ? b0 + c : p.ldb - 8;
+      offB[i] = static_cast<uint32_t>(2 * cb) + r * ldb2;
+    } else {
+      const int rb = 8 * (4 * wave + i) + (lane >> 3);
+      const int64_t gr = rb < nb - b0 ? rb : nb - b0 - 1;
+      offB[i] = static_cast<uint32_t>(2 * gr * p.ldb) + 16 * ((lane & 7) ^ row_swz(rb));
+    }
+  }
+  const char* const baseA = reinterpret_cast<const char*>(p.A) + kb * lda2;
+  const char* const baseB = reinterpret_cast<const char*>(p.B) +
+                            (TRB ? kb * ldb2 : static_cast<int64_t>(2) * (b0 * p.ldb + kb));
+  const uint32_t lds0 = lds_addr(smem) + wave * 4096;
+  // The last stage of a range may hold fewer than 64 k: rows (or chunks) past them repeat the last row
+  // (the first chunk) and meet zeros in the B fragments.
+  const int last = static_cast<int>(ke - kb - 64 * static_cast<int64_t>(nk - 1));
+  auto copy_A = [&](int s, int slot) {
+    const char* base = baseA + static_cast<int64_t>(s) * 64 * lda2;
+    const bool tail = s == nk - 1 && last < 64;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t off = offA[i];
+      if (tail) {
+        const int r = 2 * (4 * wave + i) + (lane >> 5);
+        off -= r < last ? 0u : static_cast<uint32_t>(r - last + 1) * lda2;
+      }
+      lds_dma16(base, off, lds0 + slot * TILE + i * 1024);
+    }
+  };
+  auto copy_B = [&](int s, int slot) {
+    const char* base = baseB + (TRB ? static_cast<int64_t>(s) * 64 * ldb2 : static_cast<int64_t>(s) * 128);
+    const bool tail = s == nk - 1 && last < 64;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t off = offB[i];
+      if (tail) {
+        if (TRB) {
+          const int r = 2 * (4 * wave + i) + (lane >> 5);
+          off -= r < last ? 0u : static_cast<uint32_t>(r - last + 1) * ldb2;
+        } else {
+          const int c = (lane & 7) ^ row_swz(8 * (4 * wave + i) + (lane >> 3));
+          off -= 8 * c < last ? 0u : 16u * c;
+        }
+      }
+      lds_dma16(base, off, lds0 + BOFF + slot * TILE + i * 1024);
+    }
+  };
+
+  f32x16 acc[NRA][NCB];
+#pragma unroll
+  for (int i = 0; i < NRA; ++i)
+#pragma unroll
+    for (int j = 0; j < NCB; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+
+  // Fragments. Transposing read: lane l takes rows 8 (l / 32) + (l % 16) / 4 (and 4 further) of a
+  // 16-deep k step, 8 bytes at column 16 ((l / 16) % 2) + 4 (l % 4) of a 32-column block; its row's
+  // permutation moves the block's low two bits only.
+  const int i16 = lane & 15, half = lane >> 5;
+  const int tr0 = (8 * half + (i16 >> 2)) * 512 + ((lane >> 4) & 1) * 32 + (i16 & 3) * 8;
+  int fa[NRA], fb[NCB];
+#pragma unroll
+  for (int i = 0; i < NRA; ++i) fa[i] = tr0 + 64 * ((4 * wa + i) ^ (i16 >> 2));
+#pragma unroll
+  for (int j = 0; j < NCB; ++j)
+    fb[j] = BOFF + (TRB ? tr0 + 64 * ((2 * wb + j) ^ (i16 >> 2))
+                        : (64 * wb + 32 * j + (lane & 31)) * 128);
+  const int bx = 16 * (half ^ row_swz(lane & 31));
+  bf16x8 af[2][NRA], bf[2][NCB];
+  auto load_frags = [&](int aslot, int bslot, int kk0, int left) {
+    const char* sa = smem + aslot * TILE;
+    const char* sb = smem + bslot * TILE;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+      for (int i = 0; i < NRA; ++i) {
+        const char* q = sa + fa[i] + (kk0 + ks) * 8192;
+        af[ks][i] = join(lds_read_tr(q), lds_read_tr(q + 2048));
+      }
+#pragma unroll
+      for (int j = 0; j < NCB; ++j) {
+        if constexpr (TRB) {
+          const char* q = sb + fb[j] + (kk0 + ks) * 8192;
+          bf[ks][j] = join(lds_read_tr(q), lds_read_tr(q + 2048));
+        } else {
+          bf[ks][j] = *reinterpret_cast<const bf16x8*>(sb + fb[j] + ((32 * (kk0 + ks)) ^ bx));
+        }
+      }
+    }
+    if (left < 64) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int j = 0; j < NCB; ++j)
+          bf[ks][j] = keep_first(bf[ks][j], left - 16 * (kk0 + ks) - 8 * half);
+    }
+  };
+  auto compute = [&]() {
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int i = 0; i < NRA; ++i)
+#pragma unroll
+        for (int j = 0; j < NCB; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks][i], bf[ks][j], acc[i][j], 0, 0, 0);
+  };
+
+  const int H = 2 * nk;  // turns per group
+  // Turn t: its memory half (fragments of k half t % 2 of stage s = t / 2, and the turn's copies into
+  // slots that stage s - 1 has left), a barrier, its compute half, a barrier. Group 1 runs one barrier
+  // behind group 0, so that each half of one group meets the other half of the other. At odd turns every
+  // wave waits for its own copies of stage s + 1 (all but the 4 of stage s + 2 just issued) before the
+  // barrier that opens the first memory half that reads stage s + 1.
+  auto turn = [&](int t, int a3, int b2) {  // a3 = (t / 2) % 3, b2 = (t / 2) % 2
+    const int s = t >> 1;
+    load_frags(a3, b2, (t & 1) * 2, s == nk - 1 ? last : 64);
+    if (!(t & 1)) {
+      if (t >= 2 && s + 1 < nk) copy_B(s + 1, b2 ^ 1);
+    } else {
+      if (s + 2 < nk) copy_A(s + 2, a3 == 0 ? 2 : a3 - 1);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if ((t & 1) && grp == 1) {
+      if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
+    }
+    pp_barrier();
+    compute();
+    if ((t & 1) && grp == 0) {
+      if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
+    }
+    if (!(grp == 1 && t == H - 1)) pp_barrier();
+  };
+  if (nk > 0) {
+    copy_A(0, 0);
+    copy_B(0, 0);
+    if (nk > 1) {
+      copy_A(1, 1);
+      copy_B(1, 1);
+      wait_vmcnt<8>();
+    } else {
+      wait_vmcnt<0>();
+    }
+    pp_barrier();
+    if (grp == 1) pp_barrier();
+    int a3 = 0;
+    for (int t = 0; t < H; t += 2) {
+      turn(t, a3, (t >> 1) & 1);
+      turn(t + 1, a3, (t >> 1) & 1);
+      a3 = a3 == 2 ? 0 : a3 + 1;
+    }
+  }
+
+  // No memory half reads the slots any more (group 0 passed the barrier closing the last one; group 1
+  // reads none in its last compute half) and every copy has landed, so each wave stages its stores in its
+  // own 16 KB of them.
+  store_block<NRA, NCB, PART>(acc, p, nb, b0 + 64 * wb, a0 + 128 * wa, split, lane, smem + wave * 16384);
+}
+
+// Few rows: the other operand streams past once, non-temporally. 60 rows, d = 2560, K = 151,936:
+// 128-column tiles, two workgroups to a CU, 165 us (160 non-temporal); these 136 (144 before the splits
+// took their stages in turn).
+using RingFew = RingCfg<256, 64, 4, 2, 4, 64, true>;
+using RingFew128 = RingCfg<256, 128, 4, 2, 3, 64, true>;
+// Narrow outputs, two workgroups to a CU.
+using RingNarrow = RingCfg<128, 128, 2, 2, 2>;
+using RingNarrow64 = RingCfg<128, 64, 2, 2, 3>;
+// Short sums: the stores bound the call, and three workgroups to a CU hide one another's loads and
+// stores (32768 x 4096 outputs of 256 terms 117 us with two of 64-deep stages, 104 with these).
+using RingShort = RingCfg<128, 128, 2, 2, 3, 32>;
 
 template <class C, bool TRB, bool PART>
 hipError_t launch_ring(Prod p, hipStream_t stream) {
@@ -468,9 +751,25 @@ hipError_t launch_ring(Prod p, hipStream_t stream) {
 }
 
 template <bool TRB, bool PART>
-hipError_t launch_prod(const Prod& p, hipStream_t stream) {
-  if (p.nb > 64) return launch_ring<Ring128, TRB, PART>(p, stream);
-  return launch_ring<Ring64, TRB, PART>(p, stream);
+hipError_t launch_prod(Prod p, hipStream_t stream) {
+  const ProdKind kind = prod_kind(TRB, p.na, p.nb, p.K);
+  if (kind == kProdPp) {
+    const int64_t na = (p.na + 255) / 256, nb = (p.nb + 255) / 256, n = na * nb * p.splits;
+    if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+    p.n_btiles = static_cast<int>(nb);
+    hipLaunchKernelGGL((prod_pp_kernel<TRB, PART>), dim3(static_cast<unsigned>(n)), dim3(512), 0, stream,
+                       p);
+    return hipGetLastError();
+  }
+  if constexpr (TRB) {
+    return launch_ring<RingShort, TRB, PART>(p, stream);
+  } else {
+    if (kind == kProdFew)
+      return p.nb > 64 ? launch_ring<RingFew128, TRB, PART>(p, stream)
+                       : launch_ring<RingFew, TRB, PART>(p, stream);
+    return p.nb > 64 ? launch_ring<RingNarrow, TRB, PART>(p, stream)
+                     : launch_ring<RingNarrow64, TRB, PART>(p, stream);
+  }
 }
 
 // ---------------------------------------------------------------------------------------
@@ -689,57 +988,69 @@ hipError_t launch_f32(F32Args p, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------------------------------
-// dh of every row: the sum of its parts times its scale, 0 for the rows that do not count.
+// Sum over the splits of four columns of a row's parts, eight loads in flight.
+__device__ __forceinline__ f32x4 sum_parts(const float* part, int64_t stride, int splits) {
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  int s = 0;
+  for (; s + 8 <= splits; s += 8) {
+    f32x4 u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const f32x4u*>(part + (s + i) * stride);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += u[i];
+  }
+  for (; s < splits; ++s) v += *reinterpret_cast<const f32x4u*>(part + s * stride);
+  return v;
+}
+__device__ __forceinline__ void store4(__bf16* o, f32x4 v) {
+  *reinterpret_cast<bf16x4*>(o) = bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]),
+                                         static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
+}
+
+// dh of every row: the sum of its parts times its scale, 0 for the rows that do not count. A wave takes
+// 256 columns of a row.
 template <class T>
-__global__ __launch_bounds__(256) void dh_finish_kernel(const NllArgs a, int64_t part_stride) {
+__global__ __launch_bounds__(64) void dh_finish_kernel(const NllArgs a, int64_t part_stride) {
   const int64_t m = blockIdx.x;
   const int at = a.inv[m / a.R];
   const int64_t i = static_cast<int64_t>(at) * a.R + m % a.R;
-  const float scale = at >= 0 ? a.rows[i].scale : 0.0f;
   T* out = static_cast<T*>(a.dh) + m * a.d;
-  if (sizeof(T) == 2) {
-    for (int j = 4 * threadIdx.x; j < a.d; j += 1024) {
-      f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (at >= 0) {
-        for (int s = 0; s < a.splits; ++s)
-          v += *reinterpret_cast<const f32x4*>(a.part + s * part_stride + i * a.d + j);
-        v *= scale;
-      }
-      *reinterpret_cast<bf16x4*>(out + j) =
-          bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
-                 static_cast<__bf16>(v[3])};
-    }
-  } else {
-    for (int j = threadIdx.x; j < a.d; j += 256) {
+  const int j = blockIdx.y * 256 + 4 * threadIdx.x;
+  if (j >= a.d) return;
+  const float scale = at >= 0 ? a.rows[i].scale : 0.0f;
+  if (j + 4 <= a.d) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (at >= 0) v = sum_parts(a.part + i * a.d + j, part_stride, a.splits) * scale;
+    if constexpr (sizeof(T) == 2)
+      store4(out + j, v);
+    else
+      *reinterpret_cast<f32x4u*>(out + j) = v;
+  } else {  // fp32 with d % 4 != 0
+    for (int c = j; c < a.d; ++c) {
       float v = 0.0f;
-      if (at >= 0) {
-        for (int s = 0; s < a.splits; ++s) v += a.part[s * part_stride + i * a.d + j];
-        v *= scale;
-      }
-      out[j] = static_cast<T>(v);
+      if (at >= 0)
+        for (int s = 0; s < a.splits; ++s) v += a.part[s * part_stride + i * a.d + c];
+      out[c] = static_cast<T>(at >= 0 ? v * scale : 0.0f);
     }
   }
 }
 
 // The expander's trunk gradient: the product's parts and the residual path's R branch gradients, in
-// fp32, rounded once.
-__global__ __launch_bounds__(256) void expand_dh_finish_kernel(const ExpandBackwardArgs a) {
+// fp32, rounded once. A wave takes 256 columns of a row.
+__global__ __launch_bounds__(64) void expand_dh_finish_kernel(const ExpandBackwardArgs a) {
   const int64_t p = blockIdx.x;
   const int d = a.d, R = static_cast<int>(a.R);
-  const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d;
-  for (int j = 4 * threadIdx.x; j < d; j += 1024) {
-    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < a.splits; ++s)
-      v += *reinterpret_cast<const f32x4*>(a.part + (static_cast<int64_t>(s) * a.P + p) * d + j);
-    for (int z = 0; z < R; ++z) {
-      const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d + j);
+  const int j = blockIdx.y * 256 + 4 * threadIdx.x;
+  if (j >= d) return;
+  const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d + j;
+  f32x4 v = sum_parts(a.part + p * d + j, a.P * d, a.splits);
+#pragma unroll 8
+  for (int z = 0; z < R; ++z) {
+    const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
-    }
-    *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(a.dh) + p * d + j) =
-        bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]), static_cast<__bf16>(v[2]),
-               static_cast<__bf16>(v[3])};
+    for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
   }
+  store4(static_cast<__bf16*>(a.dh) + p * d + j, v);
 }
 
 // dc: the sum over the trunk rows of every branch feature's gradient. A workgroup takes 128 features
@@ -918,11 +1229,11 @@ hipError_t launch_nll_backward(const NllArgs& a, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   if (M == 0) return hipSuccess;
-  const dim3 grid(static_cast<unsigned>(M));
+  const dim3 grid(static_cast<unsigned>(M), static_cast<unsigned>((a.d + 255) / 256));
   if (a.bf16)
-    hipLaunchKernelGGL(dh_finish_kernel<__bf16>, grid, dim3(256), 0, stream, a, part_stride);
+    hipLaunchKernelGGL(dh_finish_kernel<__bf16>, grid, dim3(64), 0, stream, a, part_stride);
   else
-    hipLaunchKernelGGL(dh_finish_kernel<float>, grid, dim3(256), 0, stream, a, part_stride);
+    hipLaunchKernelGGL(dh_finish_kernel<float>, grid, dim3(64), 0, stream, a, part_stride);
   return hipGetLastError();
 }
 
@@ -942,8 +1253,9 @@ hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t strea
     p.splits = a.splits;
     e = launch_prod<false, true>(p, stream);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(expand_dh_finish_kernel, dim3(static_cast<unsigned>(a.P)), dim3(256), 0, stream,
-                       a);
+    hipLaunchKernelGGL(expand_dh_finish_kernel,
+                       dim3(static_cast<unsigned>(a.P), static_cast<unsigned>((a.d + 255) / 256)),
+                       dim3(64), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

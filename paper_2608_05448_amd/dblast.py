@@ -7,8 +7,10 @@ kernels. There is no fallback: if the library is not built or no GPU is visible,
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import functools
+import operator
 import os
 
 import torch
@@ -526,58 +528,78 @@ def dbl_expand_branches_backward(h, W, dout, want_dh=True, want_dW=True, want_dc
 
 
 _GRAD_TYPES = {torch.float32: DBL_F32, torch.bfloat16: DBL_BF16}
+_dtype_of = operator.attrgetter("dtype")
 
 
+# A set has hundreds of tensors, so that every look at each of them counts (20 us for 245 tensors):
+# looked at in bulk, and one by one only to say what is wrong.
 def _tensors(ts, name, dev):
-    """Addresses of a list of gradients (bf16 or fp32, contiguous, on ``dev``)."""
-    for t in ts:
-        if not (t.dtype in _GRAD_TYPES and t.is_contiguous() and t.device == dev):
+    """Types, numbers of elements and addresses of a list of gradients (bf16 or fp32, contiguous, on
+    ``dev``), as arrays."""
+    types = list(map(_dtype_of, ts))
+    if not (set(types) <= _GRAD_TYPES.keys() and all(map(torch.Tensor.is_contiguous, ts))
+            and set(map(torch.Tensor.get_device, ts)) <= {dev.index}):
+        for t in ts:
             if t.dtype not in _GRAD_TYPES:
                 raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
             if not t.is_contiguous():
                 raise ValueError(f"{name} must be contiguous")
-            raise ValueError(f"{name} must be on one GPU, got {t.device} beside {dev}")
-    return (_P * len(ts))(*[t.data_ptr() for t in ts])
+            if t.device != dev:
+                raise ValueError(f"{name} must be on one GPU, got {t.device} beside {dev}")
+    return (types, array.array("q", map(torch.Tensor.numel, ts)),
+            array.array("Q", map(torch.Tensor.data_ptr, ts)))
 
 
 def _grads(grads):
     grads = list(grads)
-    dev = grads[0].device if grads else None
-    if dev is not None and dev.type != "cuda":
+    if not all(isinstance(t, torch.Tensor) for t in grads):
+        raise TypeError("grads must be torch.Tensors")
+    if not grads:
+        return grads, None, [], None, None, None
+    dev = grads[0].device
+    if dev.type != "cuda":
         raise ValueError("grads must be GPU tensors")
-    n = len(grads)
-    return (grads, dev, _tensors(grads, "grads", dev), (_I64 * n)(*[t.numel() for t in grads]),
-            (ctypes.c_int32 * n)(*[_GRAD_TYPES[t.dtype] for t in grads]))
+    types, numel, ptrs = _tensors(grads, "grads", dev)
+    return (grads, dev, types, numel, ptrs, array.array("i", map(_GRAD_TYPES.__getitem__, types)))
+
+
+def _at(a):
+    return a.buffer_info()[0]
 
 
 def dbl_grad_norm(grads, norm=None, ws=None):
     """Euclidean norm of a list of gradients (bf16 or fp32, contiguous, one GPU) taken together: a
     0-dimensional fp32 tensor on their GPU (``norm`` if given)."""
-    grads, dev, ptrs, numel, dt = _grads(grads)
+    grads, dev, types, numel, ptrs, dt = _grads(grads)
     if dev is None:
         raise ValueError("grads is empty")
     norm = torch.empty((), dtype=torch.float32, device=dev) if norm is None else norm
     _need(norm, "norm", torch.float32, ())
     ws, nws = _workspace(DBL_OP_GRAD_NORM, Shape(len(grads), 1, 1, 1, 1), dev, ws)
     _same_device(dev, norm=norm, ws=ws)
-    _run(load().dbl_grad_norm, dev, len(grads), ptrs, numel, dt, _ptr(norm), _ptr(ws), nws)
+    _run(load().dbl_grad_norm, dev, len(grads), _at(ptrs), _at(numel), _at(dt), _ptr(norm), _ptr(ws),
+         nws)
     return norm
 
 
 def dbl_clip_grads(grads, norm, max_norm, out=None):
     """Gradients times min(1, max_norm / (norm + 1e-6)): in place, or into the tensors ``out`` (same
     types and sizes). ``norm`` is a 0-dimensional fp32 GPU tensor. Returns the list of outputs."""
-    grads, dev, ptrs, numel, dt = _grads(grads)
+    grads, dev, types, numel, ptrs, dt = _grads(grads)
     if dev is None:
         return []
     _need(norm, "norm", torch.float32, ())
     _same_device(dev, norm=norm)
-    outs = grads if out is None else list(out)
-    if len(outs) != len(grads) or any(o.dtype != t.dtype or o.shape != t.shape
-                                      for o, t in zip(outs, grads)):
-        raise ValueError("out must hold a tensor of the same type and shape for every gradient")
-    to = None if out is None else _tensors(outs, "out", dev)
-    _run(load().dbl_clip_grads, dev, len(grads), ptrs, to, numel, dt, _ptr(norm), float(max_norm))
+    outs, to = grads, None
+    if out is not None:
+        outs = list(out)
+        if not all(isinstance(t, torch.Tensor) for t in outs):
+            raise TypeError("out must be torch.Tensors")
+        otypes, onumel, to = _tensors(outs, "out", dev)
+        if otypes != types or onumel != numel:
+            raise ValueError("out must hold a tensor of the same type and size for every gradient")
+    _run(load().dbl_clip_grads, dev, len(grads), _at(ptrs), None if to is None else _at(to), _at(numel),
+         _at(dt), _ptr(norm), float(max_norm))
     return outs
 
 
