@@ -464,7 +464,7 @@ dbl_status dbl_expand_branches_backward(dbl_shape shape, const void* h, const vo
  *   n       number of tensors, 0 .. 2^20 (0: norm = 0)
  *   grads   [n] device pointers, aligned to their elements (a view into a bucket may start
  *           anywhere); a tensor of 0 elements may be NULL
- *   numel   [n] numbers of elements >= 0, less than 2^44 together
+ *   numel   [n] numbers of elements >= 0, less than 2^40 together
  *   dt      [n] DBL_F32 or DBL_BF16
  *   norm    out: one fp32 (device)
  *   ws      workspace of dbl_workspace_bytes(DBL_OP_GRAD_NORM, shape) bytes, shape.B = n and 1 elsewhere

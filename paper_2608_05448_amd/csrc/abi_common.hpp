@@ -114,7 +114,7 @@ inline WsLayout layout(int op, const dbl_shape& s) {
       sizes[3] = B * K * R * static_cast<size_t>(s.d) * sizeof(float);
       n = 6;
       if (op == DBL_OP_HEAD_NLL) {
-        sizes[4] = B * K * R * nT * sizeof(float);
+        sizes[4] = B * K * R * dbl::nll_tiles(false, s.B * s.K * s.R, s.V) * sizeof(float);
         sizes[5] = B * K * R * sizeof(float);
       } else {
         const int64_t M = s.B * s.K * s.R;
@@ -122,7 +122,9 @@ inline WsLayout layout(int op, const dbl_shape& s) {
         for (int elem = 2; elem <= 4; elem += 2) {  // the call's type is not known here
           const int64_t piece = dbl::nll_piece(M, s.V, elem);
           const size_t grad = static_cast<size_t>(M) * piece * elem;
-          const size_t part = sizes[3] * dbl::grad_splits(s.d, M, piece < s.V ? piece : s.V);
+          const int64_t ids = piece < s.V ? piece : s.V;
+          const size_t part =
+              sizes[3] * (elem == 2 ? dbl::grad_splits(s.d, M, ids) : dbl::grad_splits_f32(s.d, M, ids));
           sizes[5] = sizes[5] > grad ? sizes[5] : grad;
           sizes[6] = sizes[6] > part ? sizes[6] : part;
         }

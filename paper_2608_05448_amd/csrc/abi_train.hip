@@ -78,7 +78,7 @@ dbl_status check_tensors(int64_t n, const void* const* grads, const int64_t* num
     if (dt[i] != DBL_F32 && dt[i] != DBL_BF16)
       return fail(DBL_EDTYPE, "dt must be DBL_BF16 or DBL_F32");
     if (numel[i] < 0 || numel[i] >= dbl::kMaxGradElements - all)
-      return fail(DBL_ESHAPE, "numel must be >= 0 and less than 2^44 together");
+      return fail(DBL_ESHAPE, "numel must be >= 0 and less than 2^40 together");
     all += numel[i];
     t.n = numel[i];
     t.bf16 = dt[i] == DBL_BF16;
@@ -157,7 +157,8 @@ dbl_status dbl_head_nll_backward(dbl_shape s, int dt, const void* h, const void*
     a.part = reinterpret_cast<float*>(base + L.off[6]);
     const int64_t M = s.B * s.K * s.R;
     a.piece = dbl::nll_piece(M, s.V, static_cast<int>(e));
-    a.splits = dbl::grad_splits(s.d, M, a.piece < s.V ? a.piece : s.V);
+    const int64_t ids = a.piece < s.V ? a.piece : s.V;
+    a.splits = a.bf16 ? dbl::grad_splits(s.d, M, ids) : dbl::grad_splits_f32(s.d, M, ids);
     return hip_status(dbl::launch_nll_backward(a, static_cast<hipStream_t>(stream)),
                       "head nll backward launch");
   });

@@ -1371,7 +1371,9 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
       if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
     }
     pp_barrier();
+    __builtin_amdgcn_s_setprio(1);  // the computing wave issues before its neighbour's copies and reads
     compute();
+    __builtin_amdgcn_s_setprio(0);
     if ((t & 1) && grp == 0) {
       if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
     }

@@ -265,12 +265,28 @@ inline int grad_splits(int64_t na, int64_t nb, int64_t K) {
   return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
 }
 
+// Rows up to which the fp32 kernel takes tiles of 32 rows, and the tile log-masses a row has: of 128 ids,
+// 32 in that kernel.
+constexpr int64_t kF32FewRows = 32;
+inline int64_t nll_tiles(bool bf16, int64_t M, int64_t V) {
+  const int64_t ids = !bf16 && M <= kF32FewRows ? 32 : kTile;
+  return (V + ids - 1) / ids;
+}
+
+// The splits for fp32, whose kernel has 128 x 128 tiles and 32-deep stages: small problems are bound by the
+// walk over K (a stage takes about 2 us to load), so parts have 32 terms at least.
+inline int grad_splits_f32(int64_t na, int64_t nb, int64_t K) {
+  if (na <= 0 || nb <= 0 || K <= 0) return 1;
+  const int64_t s = 512 / (((na + 127) / 128) * ((nb + 127) / 128)), most = (K + 31) / 32;
+  return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
+}
+
 constexpr int64_t kMaxTrainRows = 0x7fffffff;
 
 constexpr int kNormSet = 180;      // tensors of one launch of the gradient norm
 constexpr int kNormBlocks = 1024;  // its workgroups, and partial sums, at most
 inline int64_t norm_parts(int64_t n) { return (n + kNormSet - 1) / kNormSet * kNormBlocks; }
-constexpr int64_t kMaxGradElements = int64_t(1) << 44;  // of all tensors (chunks are numbered in 31 bits)
+constexpr int64_t kMaxGradElements = int64_t(1) << 40;  // of all tensors (chunks are numbered in 31 bits)
 
 inline int n_chunks(int nT) { return (nT + kTilesPerChunk - 1) / kTilesPerChunk; }
 

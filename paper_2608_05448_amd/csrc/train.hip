@@ -695,7 +695,9 @@ __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
       if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
     }
     pp_barrier();
+    __builtin_amdgcn_s_setprio(1);  // the computing wave issues before its neighbour's copies and reads
     compute();
+    __builtin_amdgcn_s_setprio(0);
     if ((t & 1) && grp == 0) {
       if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
     }
@@ -773,9 +775,12 @@ hipError_t launch_prod(Prod p, hipStream_t stream) {
 }
 
 // ---------------------------------------------------------------------------------------
-// fp32 GEMM: out(a, b) = sum_k A(k, a) B(k, b) on v_mfma_f32_32x32x2_f32 (fp32 products and sums).
-// 128 x 128 tile, four waves of 128 x 32, 16-deep stages staged through registers. An operand is
-// either [K, n] (TR) or [n, K] row-major; any size and 4-byte alignment.
+// fp32 GEMM: out(a, b) = sum_k A(k, a) B(k, b) on v_mfma_f32_32x32x2_f32 (fp32 products and sums). Four
+// waves, 32-deep stages staged through registers. An operand is either [K, n] (TR) or [n, K] row-major;
+// any size and 4-byte alignment. ROWS = 128: 128 x 128 tile, waves of 128 a x 32 b. ROWS = 32, for up to
+// 32 rows: 128 x 32 tile, waves of 32 a (a 128-row tile would spend its MFMAs on rows that are not there:
+// 8 rows at d = 64, V = 256 11 us, of which 4 MFMAs).
+// Tile log-masses are of a wave's ids (128 or 32).
 
 struct F32Args {
   const float* A;
@@ -801,190 +806,187 @@ struct F32Args {
 
 enum F32Epi : int { kF32Part = 0, kF32Out = 1, kF32Nll = 2, kF32Grad = 3 };
 
-template <bool TRA, bool TRB, int EPI>
+// 32 x N values of an operand in LDS as [k][i] rows of N + 4, N / 8 a thread: TR along a row of K, else
+// along K; 0 past the ends.
+template <bool TR, int N>
+struct F32Stage {
+  static constexpr int VT = N / 8, LD = N + 4;
+  f32x4 r[VT / 4];
+  __device__ __forceinline__ void load(const float* X, int64_t ld, int64_t i0, int64_t n, int64_t k0,
+                                       int64_t ke) {
+    const int tid = threadIdx.x;
+    const int64_t row = TR ? k0 + tid / 8 : i0 + tid / (32 / VT);
+    const int64_t col = TR ? i0 + VT * (tid % 8) : k0 + VT * (tid % (32 / VT));
+    const int64_t left = row < (TR ? ke : n) ? (TR ? n : ke) - col : 0;
+    const float* q = X + row * ld + col;
+    if (left >= VT) {
+#pragma unroll
+      for (int j = 0; j < VT / 4; ++j) r[j] = *reinterpret_cast<const f32x4u*>(q + 4 * j);
+    } else {
+#pragma unroll
+      for (int j = 0; j < VT; ++j) r[j / 4][j % 4] = j < left ? q[j] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ void store(float* S) const {
+    const int tid = threadIdx.x;
+    if constexpr (TR) {
+      float* q = S + (tid / 8) * LD + VT * (tid % 8);
+#pragma unroll
+      for (int j = 0; j < VT / 4; ++j) *reinterpret_cast<f32x4*>(q + 4 * j) = r[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < VT; ++j)
+        S[(VT * (tid % (32 / VT)) + j) * LD + tid / (32 / VT)] = r[j / 4][j % 4];
+    }
+  }
+};
+
+template <bool TRA, bool TRB, int EPI, int ROWS>
 __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
-  constexpr int BK = 16, LD = 132;
-  __shared__ __attribute__((aligned(16))) float As[2][BK * LD], Bs[2][BK * LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int BK = 32, NRA = ROWS == 128 ? 4 : 1, IDS = 32 * NRA;  // a of a wave
+  using SA = F32Stage<TRA, 128>;
+  using SB = F32Stage<TRB, ROWS>;
+  __shared__ __attribute__((aligned(16))) float As[2][BK * SA::LD], Bs[2][BK * SB::LD];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int half = lane >> 5;
-  int64_t K = p.count_k ? *p.count_k : p.K;
+  const int wa = ROWS == 128 ? 0 : wave * 32, wb = ROWS == 128 ? wave * 32 : 0;
+  const int64_t K = p.count_k ? *p.count_k : p.K;
   const int64_t nb = p.count_b ? *p.count_b : p.nb;
   const int n_atiles = static_cast<int>((p.na + 127) / 128);
   const int bt = blockIdx.x % p.n_btiles, rest = blockIdx.x / p.n_btiles;
   const int at = rest % n_atiles, split = rest / n_atiles;
-  const int64_t a0 = static_cast<int64_t>(at) * 128, b0 = static_cast<int64_t>(bt) * 128;
+  const int64_t a0 = static_cast<int64_t>(at) * 128, b0 = static_cast<int64_t>(bt) * ROWS;
   if (b0 >= nb) return;
   const int64_t per = ((K + p.splits - 1) / p.splits + BK - 1) / BK * BK;
   const int64_t kb = split * per < K ? split * per : K;
   const int64_t ke = kb + per < K ? kb + per : K;
 
-  // 16 x 128 values of an operand, 8 a thread: TR four and four along a row of K, else 8 along K.
-  float ra[8], rb[8];
-  auto load = [&](auto tr, const float* X, int64_t ld, int64_t i0, int64_t n, int64_t k0, float (&r)[8]) {
-    if constexpr (decltype(tr)::value) {
-      const int64_t k = k0 + tid / 16;
-      const int64_t i = i0 + 8 * (tid % 16);
+  f32x16 acc[NRA];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j] = 0.0f;
-      if (k < ke) {
-        const float* q = X + k * ld + i;
-        if (i + 8 <= n) {
-          const f32x4u u = *reinterpret_cast<const f32x4u*>(q), v = *reinterpret_cast<const f32x4u*>(q + 4);
+  for (int i = 0; i < NRA; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            r[j] = u[j];
-            r[4 + j] = v[j];
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (i + j < n) r[j] = q[j];
-        }
-      }
-    } else {
-      const int64_t k = k0 + 8 * (tid & 1);
-      const int64_t i = i0 + tid / 2;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) r[j] = 0.0f;
-      if (i < n) {
-        const float* q = X + i * ld + k;
-        if (k + 8 <= ke) {
-          const f32x4u u = *reinterpret_cast<const f32x4u*>(q), v = *reinterpret_cast<const f32x4u*>(q + 4);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            r[j] = u[j];
-            r[4 + j] = v[j];
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (k + j < ke) r[j] = q[j];
-        }
-      }
-    }
-  };
-  auto store = [&](auto tr, float* S, const float (&r)[8]) {
-    if constexpr (decltype(tr)::value) {
-      float* q = S + (tid / 16) * LD + 8 * (tid % 16);
-      *reinterpret_cast<f32x4*>(q) = f32x4{r[0], r[1], r[2], r[3]};
-      *reinterpret_cast<f32x4*>(q + 4) = f32x4{r[4], r[5], r[6], r[7]};
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) S[(8 * (tid & 1) + j) * LD + tid / 2] = r[j];
-    }
-  };
-  using TA = std::integral_constant<bool, TRA>;
-  using TB = std::integral_constant<bool, TRB>;
-
-  f32x16 acc[4][1];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) acc[i][0][r] = 0.0f;
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.0f;
 
   if (kb < ke) {
-    load(TA{}, p.A, p.lda, a0, p.na, kb, ra);
-    load(TB{}, p.B, p.ldb, b0, nb, kb, rb);
-    store(TA{}, As[0], ra);
-    store(TB{}, Bs[0], rb);
+    SA ra;
+    SB rb;
+    ra.load(p.A, p.lda, a0, p.na, kb, ke);
+    rb.load(p.B, p.ldb, b0, nb, kb, ke);
+    ra.store(As[0]);
+    rb.store(Bs[0]);
     __syncthreads();
     int buf = 0;
     for (int64_t k0 = kb; k0 < ke; k0 += BK, buf ^= 1) {
       const bool more = k0 + BK < ke;
       if (more) {
-        load(TA{}, p.A, p.lda, a0, p.na, k0 + BK, ra);
-        load(TB{}, p.B, p.ldb, b0, nb, k0 + BK, rb);
+        ra.load(p.A, p.lda, a0, p.na, k0 + BK, ke);
+        rb.load(p.B, p.ldb, b0, nb, k0 + BK, ke);
       }
-      const float* sa = As[buf] + (lane & 31);
-      const float* sb = Bs[buf] + wave * 32 + (lane & 31);
+      const float* sa = As[buf] + wa + (lane & 31);
+      const float* sb = Bs[buf] + wb + (lane & 31);
 #pragma unroll
       for (int kk = 0; kk < BK; kk += 2) {
-        const float b = sb[(kk + half) * LD];
+        const float b = sb[(kk + half) * SB::LD];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          acc[i][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(sa[(kk + half) * LD + 32 * i], b, acc[i][0],
-                                                           0, 0, 0);
+        for (int i = 0; i < NRA; ++i)
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(sa[(kk + half) * SA::LD + 32 * i], b, acc[i], 0,
+                                                        0, 0);
       }
       if (more) {
-        store(TA{}, As[buf ^ 1], ra);
-        store(TB{}, Bs[buf ^ 1], rb);
+        ra.store(As[buf ^ 1]);
+        rb.store(Bs[buf ^ 1]);
       }
       __syncthreads();
     }
   }
 
-  const int64_t b = b0 + wave * 32 + (lane & 31);
+  // Lane l holds b = l % 32 of its wave's and, in registers 4 g .. 4 g + 3 of block i, a = 32 i + 8 g +
+  // 4 (l / 32) + {0 .. 3}.
+  const int64_t b = b0 + wb + (lane & 31), aw = a0 + wa;
   if constexpr (EPI == kF32Part || EPI == kF32Out) {
     if (b >= nb) return;
+    float* const row = EPI == kF32Part ? p.part + split * p.part_stride + b * p.na : p.out + b * p.na;
+    const bool add = EPI == kF32Part && p.accumulate;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < NRA; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int64_t a = a0 + 32 * i + 8 * (r >> 2) + 4 * half + (r & 3);
-        if (a >= p.na) continue;
-        if constexpr (EPI == kF32Part) {
-          float* o = p.part + split * p.part_stride + b * p.na + a;
-          *o = acc[i][0][r] + (p.accumulate ? *o : 0.0f);
+      for (int g = 0; g < 4; ++g) {
+        const int64_t a = aw + 32 * i + 8 * g + 4 * half;
+        f32x4 v = {acc[i][4 * g], acc[i][4 * g + 1], acc[i][4 * g + 2], acc[i][4 * g + 3]};
+        if (a + 4 <= p.na) {
+          f32x4u* o = reinterpret_cast<f32x4u*>(row + a);
+          if (add) v += *o;
+          *o = v;
         } else {
-          p.out[b * p.na + a] = acc[i][0][r];
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            if (a + q < p.na) row[a + q] = v[q] + (add ? row[a + q] : 0.0f);
         }
       }
   } else {
-    // a: ids of one vocabulary tile, b: rows (the lane layout of the bf16 head's epilogues).
-    const int lim = static_cast<int>(p.na - a0 < 128 ? p.na - a0 : 128) - 4 * half;
+    // a: ids, b: rows (the lane layout of the bf16 head's epilogues).
+    if (aw >= p.na) return;
+    const int lim = static_cast<int>(p.na - aw < IDS ? p.na - aw : IDS) - 4 * half;
     if constexpr (EPI == kF32Nll) {
-      float x[64];
+      float x[16 * NRA];
 #pragma unroll
-      for (int i = 0; i < 64; ++i)
-        x[i] = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) < lim ? acc[i >> 4][0][i & 15] : -INFINITY;
-      const int64_t o = b < nb ? p.rows[b].token - a0 - 4 * half : -1;
+      for (int i = 0; i < 16 * NRA; ++i)
+        x[i] = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) < lim ? acc[i >> 4][i & 15] : -INFINITY;
+      const int64_t o = b < nb ? p.rows[b].token - aw - 4 * half : -1;
       if (o >= 0 && o < lim && !(o & 4)) {
         float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 64; ++i)
+        for (int i = 0; i < 16 * NRA; ++i)
           t = o == 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) ? x[i] : t;
         p.tgt[b] = t;
       }
       float mx = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < 64; ++i) mx = fmaxf(mx, x[i]);
+      for (int i = 0; i < 16 * NRA; ++i) mx = fmaxf(mx, x[i]);
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       float s = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 64; ++i) s += __expf(x[i] - mx);
+      for (int i = 0; i < 16 * NRA; ++i) s += __expf(x[i] - mx);
       s += __shfl_xor(s, 32);
-      if (b < nb && half == 0) p.lmass[b * p.nT + a0 / 128] = mx + logf(s);
+      if (b < nb && half == 0) p.lmass[b * p.nT + aw / IDS] = mx + logf(s);
     } else {
       if (b >= nb) return;
       const TrainRow row = p.rows[b];
-      const int64_t o = row.token - p.vbase - a0 - 4 * half;
+      const int64_t o = row.token - p.vbase - aw - 4 * half;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < NRA; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           f32x4 y;
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const int at0 = 32 * i + 8 * g + q;
-            float u = expf(acc[i][0][4 * g + q] - row.shift);
+            float u = expf(acc[i][4 * g + q] - row.shift);
             u = o == at0 ? row.at_token : u;
             y[q] = at0 < lim ? u : 0.0f;
           }
-          *reinterpret_cast<f32x4*>(p.grad + b * p.ldg + a0 + 32 * i + 8 * g + 4 * half) = y;
+          *reinterpret_cast<f32x4*>(p.grad + b * p.ldg + aw + 32 * i + 8 * g + 4 * half) = y;
         }
     }
   }
 }
 
-template <bool TRA, bool TRB, int EPI>
-hipError_t launch_f32(F32Args p, hipStream_t stream) {
-  const int64_t na = (p.na + 127) / 128, nb = (p.nb + 127) / 128;
+template <bool TRA, bool TRB, int EPI, int ROWS>
+hipError_t launch_f32_rows(F32Args p, hipStream_t stream) {
+  const int64_t na = (p.na + 127) / 128, nb = (p.nb + ROWS - 1) / ROWS;
   const int64_t n = na * nb * p.splits;
   if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
   p.n_btiles = static_cast<int>(nb);
-  hipLaunchKernelGGL((gemm_f32_kernel<TRA, TRB, EPI>), dim3(static_cast<unsigned>(n)), dim3(256), 0,
+  hipLaunchKernelGGL((gemm_f32_kernel<TRA, TRB, EPI, ROWS>), dim3(static_cast<unsigned>(n)), dim3(256), 0,
                      stream, p);
   return hipGetLastError();
+}
+
+template <bool TRA, bool TRB, int EPI>
+hipError_t launch_f32(const F32Args& p, hipStream_t stream) {
+  if constexpr (!TRB)  // the products over the rows have the vocabulary there, many ids
+    if (p.nb <= kF32FewRows) return launch_f32_rows<TRA, TRB, EPI, 32>(p, stream);
+  return launch_f32_rows<TRA, TRB, EPI, 128>(p, stream);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1092,7 +1094,7 @@ __global__ __launch_bounds__(1024) void expand_dc_kernel(const __bf16* __restric
 
 hipError_t launch_nll(const NllArgs& a, hipStream_t stream) {
   const int64_t M = a.P * a.R;
-  const int nT = static_cast<int>((a.V + kTile - 1) / kTile);
+  const int nT = static_cast<int>(nll_tiles(a.bf16, M, a.V));
   hipError_t e = gather_rows(a, stream);
   if (e != hipSuccess) return e;
   if (a.bf16) {
