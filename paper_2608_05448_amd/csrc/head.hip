@@ -337,6 +337,12 @@ struct EpiArgs {
 
 constexpr bool epi_train(int epi) { return epi == kEpiNll || epi == kEpiGrad; }
 
+// A fragment (8 units of a 16-deep k step, the upper half of the wave the second 8) of a step of which
+// `left` units are there, a multiple of 8: 0 where they are not.
+__device__ __forceinline__ bf16x8 first_units(bf16x8 v, int left, int lane) {
+  return 8 * (lane >> 5) < left ? v : bf16x8{};
+}
+
 // Epilogue of dbl_head_nll: tile log-mass as in the head's epilogues (the same arithmetic as
 // tile_logsoftmax_store_lds), and the token's logit from the one lane that holds it.
 template <int NRB, int NCB>
@@ -378,10 +384,10 @@ __device__ __forceinline__ void tile_nll_store(f32x16 (&acc)[NRB][NCB], const Ep
 }
 
 // Epilogue of dbl_head_nll_backward: the logits' gradient of a row over its scale, in bf16 (see
-// TrainRow): exp(logit - lse) / q for every id but the token, -1 for the token; 0 for the ids of a tile past V. With xp (8 KB of LDS of this wave) 32
-// rows x 128 ids at a time go through LDS, so that a store instruction writes four whole 256-byte row
-// segments (16-byte chunk c of row r at chunk c ^ (r % 16)); without, 8 bytes a lane.
-template <int NRB, int NCB, bool LDS>
+// TrainRow): exp(logit - lse) / q for every id but the token, -1 for the token; 0 for the ids of a tile past V. 32 rows
+// x 128 ids at a time go through xp (8 KB of LDS of this wave), so that a store instruction writes four
+// whole 256-byte row segments (16-byte chunk c of row r at chunk c ^ (r % 16)).
+template <int NRB, int NCB>
 __device__ __forceinline__ void tile_grad_store(f32x16 (&acc)[NRB][NCB], const EpiArgs& e, int64_t M,
                                                 int64_t V, int64_t v0w, int64_t m0w, int lane,
                                                 char* xp) {
@@ -408,26 +414,21 @@ __device__ __forceinline__ void tile_grad_store(f32x16 (&acc)[NRB][NCB], const E
           p = o == at ? row.at_token : p;
           y[q] = static_cast<__bf16>(at < lim ? p : 0.0f);
         }
-        if constexpr (LDS)
-          *reinterpret_cast<bf16x4*>(xp + lr * 256 + (((rb * 4 + g) ^ (lr & 15)) * 16) + half * 8) = y;
-        else if (m < M)
-          *reinterpret_cast<bf16x4*>(grad + m * e.ldg + v0w + 32 * rb + 8 * g + 4 * half) = y;
+        *reinterpret_cast<bf16x4*>(xp + lr * 256 + (((rb * 4 + g) ^ (lr & 15)) * 16) + half * 8) = y;
       }
-    if constexpr (LDS) {
-      // Wave-private LDS region: the writes above precede these reads in the wave's LDS queue.
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    // Wave-private LDS region: the writes above precede these reads in the wave's LDS queue.
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-      for (int jj = 0; jj < 8; ++jj) {
-        const int rr = 4 * jj + (lane >> 4);
-        const u32x4 y =
-            *reinterpret_cast<const u32x4*>(xp + rr * 256 + (((lane & 15) ^ (rr & 15)) * 16));
-        const int64_t mm = m0w + cb * 32 + rr;
-        if (mm < M) *reinterpret_cast<u32x4*>(grad + mm * e.ldg + v0w + 8 * (lane & 15)) = y;
-      }
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    for (int jj = 0; jj < 8; ++jj) {
+      const int rr = 4 * jj + (lane >> 4);
+      const u32x4 y =
+          *reinterpret_cast<const u32x4*>(xp + rr * 256 + (((lane & 15) ^ (rr & 15)) * 16));
+      const int64_t mm = m0w + cb * 32 + rr;
+      if (mm < M) *reinterpret_cast<u32x4*>(grad + mm * e.ldg + v0w + 8 * (lane & 15)) = y;
     }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   }
 }
 
@@ -507,10 +508,6 @@ __global__ __launch_bounds__(C::kThreads, 1) void head_bf16_kernel(
   tile_of(xcd_remap(blockIdx.x, gridDim.x), gridDim.x / n_mtiles, n_mtiles, &vt, &mt);
   const int64_t v0 = static_cast<int64_t>(vt) * C::BV;
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
-  if constexpr (epi_train(EPI)) {
-    M = *ea.count;
-    if (m0 >= M) return;
-  }
 
   // Staging: thread chunk c -> row c / CPR, 16-byte column c % CPR.
   const __bf16* a_src[C::A_CHUNKS];
@@ -622,13 +619,8 @@ __global__ __launch_bounds__(C::kThreads, 1) void head_bf16_kernel(
 
   const int64_t v0w = v0 + wv * kVTile;
   if (v0w >= V) return;
-  if constexpr (EPI == kEpiNll)
-    tile_nll_store<C::NRB, C::NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
-  else if constexpr (EPI == kEpiGrad)
-    tile_grad_store<C::NRB, C::NCB, false>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, nullptr);
-  else
-    tile_logsoftmax_store<C::NRB, C::NCB, EPI == kEpiLogSoftmaxArgmax>(
-        acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane, ea.vec4);
+  tile_logsoftmax_store<C::NRB, C::NCB, EPI == kEpiLogSoftmaxArgmax>(
+      acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane, ea.vec4);
 }
 
 // Every kernel that can serve a shape adds a row's products in the same order, 16 hidden units at a
@@ -803,10 +795,6 @@ __global__ __launch_bounds__(C::kThreads, C::kWgPerCu) void head_bf16_dma_kernel
   tile_of(xcd_remap(blockIdx.x, gridDim.x), gridDim.x / n_mtiles, n_mtiles, &vt, &mt);
   const int64_t v0 = static_cast<int64_t>(vt) * C::BV;
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
-  if constexpr (epi_train(EPI)) {
-    M = *ea.count;
-    if (m0 >= M) return;
-  }
 
   // DMA sources: instruction i of this wave covers tile rows (wave * INST + i) * RPI + [0, RPI);
   // lane -> row lane / CPR of it and the chunk whose permuted slot is lane % CPR. Addresses are
@@ -972,10 +960,6 @@ __global__ __launch_bounds__(C::kThreads, C::kWgPerCu) void head_bf16_dma_kernel
   if (v0w >= V) return;
   if constexpr (EPI == kEpiExpand)
     expand_store<C::NRB, C::NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
-  else if constexpr (EPI == kEpiNll)
-    tile_nll_store<C::NRB, C::NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
-  else if constexpr (EPI == kEpiGrad)
-    tile_grad_store<C::NRB, C::NCB, false>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, nullptr);
   else
     tile_logsoftmax_store<C::NRB, C::NCB, EPI == kEpiLogSoftmaxArgmax>(
         acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane, ea.vec4);
@@ -1253,7 +1237,9 @@ __device__ __forceinline__ void pp_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <int EPI>
+// TAIL: d % 8 == 0 only. The last stage holds `last` < 64 units: chunks past them fetch the row's first
+// chunk of the stage, and meet zeros in the branch rows' fragments.
+template <int EPI, bool TAIL = false>
 __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
     const __bf16* __restrict__ h, const __bf16* __restrict__ w, const EpiArgs ea, int64_t M,
     int64_t V, int d, int n_mtiles) {
@@ -1295,20 +1281,30 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
     offB[i] = static_cast<uint32_t>(gb * d * 2 + c * 16);
   }
   const uint32_t lds_row = lds_addr(smem) + (16 * grp + 4 * q) * 1024;
-  const int nk = d / C::BK;
+  const int nk = TAIL ? (d + C::BK - 1) / C::BK : d / C::BK;
+  const int last = TAIL ? d - (nk - 1) * C::BK : C::BK;
   const int k0 = walk_start<false>(EPI == kEpiGrad ? v0 + ea.vbase : v0, d) / C::BK;
+  // How far copy i's chunk is moved back, to the stage's first.
+  auto past = [&](int s, int i) -> uint32_t {
+    if constexpr (TAIL) {
+      const int c = (lane % 8) ^ dma_swz<8>(128 * grp + (4 * q + i) * 8 + lane / 8);
+      return s == nk - 1 && 8 * c >= last ? 16u * c : 0u;
+    }
+    return 0u;
+  };
   auto copy_A = [&](int s, int slot) {
     s = s + k0 < nk ? s + k0 : s + k0 - nk;
     const char* base = srcA + static_cast<int64_t>(s) * (2 * C::BK);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) lds_dma16(base, offA[i], lds_row + slot * TILE + i * 1024);
+    for (int i = 0; i < 4; ++i)
+      lds_dma16(base, offA[i] - past(s, i), lds_row + slot * TILE + i * 1024);
   };
   auto copy_B = [&](int s, int slot) {
     s = s + k0 < nk ? s + k0 : s + k0 - nk;
     const char* base = srcB + static_cast<int64_t>(s) * (2 * C::BK);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      lds_dma16(base, offB[i], lds_row + BOFF + slot * TILE + i * 1024);
+      lds_dma16(base, offB[i] - past(s, i), lds_row + BOFF + slot * TILE + i * 1024);
   };
 
   f32x16 acc[NRB][NCB];
@@ -1325,7 +1321,7 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
   const int a_base = (wv * kVTile + (lane & 31)) * ROWB;
   const int b_base = BOFF + (wm * C::TM + (lane & 31)) * ROWB;
   bf16x8 af[2][NRB], bfr[2][NCB];
-  auto load_frags = [&](int aslot, int bslot, int kk0) {
+  auto load_frags = [&](int aslot, int bslot, int kk0, int left) {
     const char* sa = smem + aslot * TILE;
     const char* sb = smem + bslot * TILE;
 #pragma unroll
@@ -1338,6 +1334,14 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
       for (int cb = 0; cb < NCB; ++cb)
         bfr[ks][cb] = *reinterpret_cast<const bf16x8*>(sb + b_base + cb * 32 * ROWB + x);
     }
+    if constexpr (TAIL)
+      if (left < C::BK) {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int cb = 0; cb < NCB; ++cb)
+            bfr[ks][cb] = first_units(bfr[ks][cb], left - 16 * (kk0 + ks), lane);
+      }
   };
   auto compute = [&]() {
 #pragma unroll
@@ -1360,7 +1364,7 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
   // last memory half reading it.
   auto turn = [&](int t, int a3, int b2) {  // a3 = (t / 2) % 3, b2 = (t / 2) % 2
     const int s = t >> 1;
-    load_frags(a3, b2, (t & 1) * 2);
+    load_frags(a3, b2, (t & 1) * 2, s == nk - 1 ? last : C::BK);
     if (!(t & 1)) {
       if (t >= 2 && s + 1 < nk) copy_B(s + 1, b2 ^ 1);
     } else {
@@ -1408,7 +1412,7 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
   if constexpr (EPI == kEpiNll)
     tile_nll_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
   else if constexpr (EPI == kEpiGrad)
-    tile_grad_store<NRB, NCB, true>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 16384);
+    tile_grad_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 16384);
   else
     tile_logsoftmax_store_lds<NRB, NCB, EPI == kEpiLogSoftmaxArgmax>(
         acc, ea.tls, ea.lmass, ea.amax, M, V, ea.nT, v0w, m0 + wm * C::TM, lane,
@@ -1443,7 +1447,8 @@ struct FewCfg {
   static_assert(kLds <= 160 * 1024, "LDS per CU");
 };
 
-template <class C, int EPI>
+// TAIL: d % 8 == 0 only, as in the ping-pong kernel.
+template <class C, int EPI, bool TAIL = false>
 __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_kernel(
     const __bf16* __restrict__ h, const __bf16* __restrict__ w, const EpiArgs ea, int64_t M,
     int64_t V, int d, int n_mtiles) {
@@ -1483,7 +1488,16 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
     offB[i] = static_cast<uint32_t>(gr * d * 2 + ((lane % 8) ^ dma_swz<8>(r)) * 16);
   }
   const uint32_t lds0 = lds_addr(smem);
-  const int nk = d / (64 * C::KB);
+  static_assert(!TAIL || C::KB == 1, "a partial stage is one partial block");
+  const int nk = TAIL ? (d + 63) / 64 : d / (64 * C::KB);
+  const int last = TAIL ? d - (nk - 1) * 64 : 64;
+  auto past = [&](int s, int row_group) -> uint32_t {
+    if constexpr (TAIL) {
+      const int c = (lane % 8) ^ dma_swz<8>(row_group * 8 + lane / 8);
+      return s == nk - 1 && 8 * c >= last ? 16u * c : 0u;
+    }
+    return 0u;
+  };
   const int r0 = walk_start<EPI == kEpiExpand>(EPI == kEpiGrad ? v0 + ea.vbase : v0, d) / (64 * C::KB);
   auto copy = [&](int s, int slot) {
     s = s + r0 < nk ? s + r0 : s + r0 - nk;
@@ -1493,10 +1507,10 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
       const int64_t at = (static_cast<int64_t>(s) * C::KB + kb) * 128;
 #pragma unroll
       for (int i = 0; i < AW; ++i)
-        lds_dma16_wait<true>(srcA + at, offA[i], to + kb * C::BLK + (wave * AW + i) * 1024);
+        lds_dma16_wait<true>(srcA + at, offA[i] - past(s, wave * AW + i), to + kb * C::BLK + (wave * AW + i) * 1024);
 #pragma unroll
       for (int i = 0; i < BW; ++i)
-        lds_dma16_wait<false>(srcB + at, offB[i],
+        lds_dma16_wait<false>(srcB + at, offB[i] - past(s, wave * BW + i),
                        to + kb * C::BLK + C::BV * ROWB + (wave * BW + i) * 1024);
     }
   };
@@ -1539,6 +1553,11 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
 #pragma unroll
       for (int cb = 0; cb < NCB; ++cb)
         bfr[cb] = *reinterpret_cast<const bf16x8*>(blk + b_base + cb * 32 * ROWB + x);
+      if constexpr (TAIL)
+        if (kt == nk - 1) {
+#pragma unroll
+          for (int cb = 0; cb < NCB; ++cb) bfr[cb] = first_units(bfr[cb], last - 16 * ks, lane);
+        }
 #pragma unroll
       for (int rb = 0; rb < NRB; ++rb)
 #pragma unroll
@@ -1559,7 +1578,7 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
     tile_nll_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
   } else if constexpr (EPI == kEpiGrad) {
     static_assert(C::NW * 8192 <= C::kLds, "8 KB of the ring per wave that stores");
-    tile_grad_store<NRB, NCB, true>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 8192);
+    tile_grad_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 8192);
   } else {
     static_assert(C::TV == kVTile && C::WV * C::WM * 16384 <= C::kLds,
                   "head epilogue: 16 KB of the ring per wave that stores");
@@ -1758,32 +1777,41 @@ using HeadFew64 = FewCfg<256, 64, 2, 2, 1, 3>;
 using HeadFew64Short = FewCfg<128, 64, 1, 2, 1, 3>;
 using HeadFew128 = FewCfg<256, 128, 2, 4, 1, 3>;
 
-// Needs d % (64 C::KB) == 0: whole stages (both dispatchers see to it).
-template <class C, int EPI>
+// Needs d % (64 C::KB) == 0, or TAIL (the dispatchers see to it).
+template <class C, int EPI, bool TAIL = false>
 hipError_t launch_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64_t M, int64_t V,
                       int d, hipStream_t stream) {
   const int64_t dm = (M + C::BM - 1) / C::BM;
   const int64_t nwg = ((V + C::BV - 1) / C::BV) * dm;
   if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((head_bf16_few_kernel<C, EPI>), dim3(static_cast<unsigned>(nwg)),
+  hipLaunchKernelGGL((head_bf16_few_kernel<C, EPI, TAIL>), dim3(static_cast<unsigned>(nwg)),
                      dim3(C::kThreads), 0, stream, h, w, ea, M, V, d, static_cast<int>(dm));
   return hipGetLastError();
 }
 
-// The head's GEMM with the kernel that its shape takes.
+// Up to 128 rows the weight's stream bounds the call and a 256-row tile would be mostly padding.
+// V = 151,936, with the LSE launch: 60 rows at d = 2560 203 -> 149 us, 120 rows 212 -> 176, 60 rows
+// at d = 4096 300 -> 217, 120 rows 306 -> 242; from 129 rows on two 128-row tiles would stream the
+// weight twice (180 rows at d = 2560 264 us against the ping-pong kernel's 215).
+constexpr int64_t kFewRows = 128;
+template <int EPI, bool TAIL>
+hipError_t launch_head_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64_t M, int64_t V,
+                           int d, hipStream_t stream) {
+  if (M > HeadFew64::BM) return launch_few<HeadFew128, EPI, TAIL>(h, w, ea, M, V, d, stream);
+  if ((V + HeadFew64::BV - 1) / HeadFew64::BV >= kFewTiles)
+    return launch_few<HeadFew64, EPI, TAIL>(h, w, ea, M, V, d, stream);
+  return launch_few<HeadFew64Short, EPI, TAIL>(h, w, ea, M, V, d, stream);
+}
+
+// The head's GEMM with the kernel that its shape takes. The training epilogues have no kernels of their
+// own for d % 64 != 0: the others' take a partial last stage (168 rows at d = 1000 against 50,257 ids
+// 63 us in the register-staged kernel).
 template <int EPI>
 hipError_t launch_head_gemm(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64_t M, int64_t V,
                             int d, hipStream_t stream) {
-  // Up to 128 rows the weight's stream bounds the call and a 256-row tile would be mostly padding.
-  // V = 151,936, with the LSE launch: 60 rows at d = 2560 203 -> 149 us, 120 rows 212 -> 176, 60 rows
-  // at d = 4096 300 -> 217, 120 rows 306 -> 242; from 129 rows on two 128-row tiles would stream the
-  // weight twice (180 rows at d = 2560 264 us against the ping-pong kernel's 215).
-  if (d % 64 == 0 && M <= 128) {
-    return M > HeadFew64::BM ? launch_few<HeadFew128, EPI>(h, w, ea, M, V, d, stream)
-           : (V + HeadFew64::BV - 1) / HeadFew64::BV >= kFewTiles
-               ? launch_few<HeadFew64, EPI>(h, w, ea, M, V, d, stream)
-               : launch_few<HeadFew64Short, EPI>(h, w, ea, M, V, d, stream);
-  }
+  if (d % 64 == 0 && M <= kFewRows) return launch_head_few<EPI, false>(h, w, ea, M, V, d, stream);
+  if constexpr (epi_train(EPI))
+    if (M <= kFewRows) return launch_head_few<EPI, true>(h, w, ea, M, V, d, stream);
   static_assert(PpCfg::BM == 256 && PpCfg::BV == 256 && DCfg::BM == 256 && DCfg::BV == 256 &&
                     Cfg::BM == 256 && Cfg::BV == 256, "one grid for the 256 x 256 tiles");
   const int64_t dm = (M + 255) / 256;
@@ -1791,15 +1819,20 @@ hipError_t launch_head_gemm(const __bf16* h, const __bf16* w, const EpiArgs& ea,
   if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<unsigned>(nwg));
   const int n_mtiles = static_cast<int>(dm);
-  if (d % PpCfg::BK == 0)
+  if (d % PpCfg::BK == 0) {
     hipLaunchKernelGGL(head_bf16_pp_kernel<EPI>, grid, dim3(PpCfg::kThreads), 0, stream, h, w, ea, M,
                        V, d, n_mtiles);
-  else if (d % DCfg::BK == 0)
-    hipLaunchKernelGGL((head_bf16_dma_kernel<DCfg, EPI>), grid, dim3(DCfg::kThreads), 0, stream, h, w,
+  } else if constexpr (epi_train(EPI)) {
+    hipLaunchKernelGGL((head_bf16_pp_kernel<EPI, true>), grid, dim3(PpCfg::kThreads), 0, stream, h, w,
                        ea, M, V, d, n_mtiles);
-  else
-    hipLaunchKernelGGL((head_bf16_kernel<Cfg, EPI>), grid, dim3(Cfg::kThreads), 0, stream, h, w, ea,
-                       M, V, d, n_mtiles);
+  } else {
+    if (d % DCfg::BK == 0)
+      hipLaunchKernelGGL((head_bf16_dma_kernel<DCfg, EPI>), grid, dim3(DCfg::kThreads), 0, stream, h, w,
+                         ea, M, V, d, n_mtiles);
+    else
+      hipLaunchKernelGGL((head_bf16_kernel<Cfg, EPI>), grid, dim3(Cfg::kThreads), 0, stream, h, w, ea,
+                         M, V, d, n_mtiles);
+  }
   return hipGetLastError();
 }
 
