@@ -266,18 +266,18 @@ inline int grad_splits(int64_t na, int64_t nb, int64_t K) {
 }
 
 // Rows up to which the fp32 kernel takes tiles of 32 rows, and the tile log-masses a row has: of 128 ids,
-// 32 in that kernel.
+// in fp32 of 64, and of 32 in that kernel.
 constexpr int64_t kF32FewRows = 32;
 inline int64_t nll_tiles(bool bf16, int64_t M, int64_t V) {
-  const int64_t ids = !bf16 && M <= kF32FewRows ? 32 : kTile;
+  const int64_t ids = bf16 ? kTile : M <= kF32FewRows ? 32 : 64;
   return (V + ids - 1) / ids;
 }
 
-// The splits for fp32, whose kernel has 128 x 128 tiles and 32-deep stages: small problems are bound by the
+// The splits for fp32, whose kernel has 128 x 64 tiles and 32-deep stages: small problems are bound by the
 // walk over K (a stage takes about 2 us to load), so parts have 32 terms at least.
 inline int grad_splits_f32(int64_t na, int64_t nb, int64_t K) {
   if (na <= 0 || nb <= 0 || K <= 0) return 1;
-  const int64_t s = 512 / (((na + 127) / 128) * ((nb + 127) / 128)), most = (K + 31) / 32;
+  const int64_t s = 768 / (((na + 127) / 128) * ((nb + 63) / 64)), most = (K + 31) / 32;
   return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
 }
 

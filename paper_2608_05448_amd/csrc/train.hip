@@ -281,9 +281,11 @@ __device__ __forceinline__ int row_swz(int r) { return (r >> 1) & 7; }
 // instruction writes whole row segments (the register layout would write 8 or 16 bytes of 32 rows): lane
 // l holds row l % 32 and, in registers 4 g .. 4 g + 3 of block i, columns 32 i + 8 g + 4 (l / 32) + {0 .. 3}.
 // xp: 32 rows of 32 NRA values of LDS that no other wave touches. Chunks of a row are permuted by the row.
-template <int NRA, int NCB, bool PART>
+enum ProdOut : int { kOutPart = 0, kOutKeep = 1, kOutStream = 2 };  // fp32 sums; bf16; bf16 past the caches
+template <int NRA, int NCB, int OUT>
 __device__ __forceinline__ void store_block(f32x16 (&acc)[NRA][NCB], const Prod& p, int64_t nb,
                                             int64_t b0, int64_t a0, int split, int lane, char* xp) {
+  constexpr bool PART = OUT == kOutPart;
   constexpr int COLS = 32 * NRA, ROWB = COLS * (PART ? 4 : 2), CH = ROWB / 16;  // 16-byte chunks a row
   constexpr int RPI = 64 / CH;                                                // rows per instruction
   static_assert(CH >= 4 && CH <= 64 && (CH & (CH - 1)) == 0, "whole rows per instruction");
@@ -320,7 +322,12 @@ __device__ __forceinline__ void store_block(f32x16 (&acc)[NRA][NCB], const Prod&
           if (p.accumulate) v += *o;
           *o = v;
         } else {
-          *reinterpret_cast<u32x4*>(p.out + b * p.na + a) = *reinterpret_cast<const u32x4*>(at);
+          const u32x4 v = *reinterpret_cast<const u32x4*>(at);
+          u32x4* o = reinterpret_cast<u32x4*>(p.out + b * p.na + a);
+          if constexpr (OUT == kOutStream)
+            __builtin_nontemporal_store(v, o);
+          else
+            *o = v;
         }
       }
     }
@@ -360,13 +367,14 @@ struct RingCfg {
   static constexpr int PER = AI + BI;
   static constexpr int kLds = S * STAGE;
   static constexpr int kWgPerCu = 160 * 1024 / kLds;
-  static constexpr int kWavesPerEu = kWgPerCu * NW / 4 < 1 ? 1 : kWgPerCu * NW / 4;
+  static constexpr int kWaves = kWgPerCu * NW / 4;
+  static constexpr int kWavesPerEu = kWaves < 1 ? 1 : kWaves > 4 ? 4 : kWaves;
   static_assert(TILEA % (1024 * NW) == 0 && TILEB % (1024 * NW) == 0, "whole copies");
   static_assert(NRA >= 1 && NCB >= 1 && BA % (32 * WA) == 0 && BB % (32 * WB) == 0, "tiling");
   static_assert((S - 1) * PER <= 63 && kLds <= 160 * 1024, "ring");
 };
 
-template <class C, bool TRB, bool PART>
+template <class C, bool TRB, int OUT>
 __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(const Prod p) {
   constexpr int BA = C::BA, BB = C::BB, NRA = C::NRA, NCB = C::NCB, BK = C::BK;
   static_assert(TRB || BK == 64, "an operand held along K has 128-byte LDS rows");
@@ -511,9 +519,9 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
 
   // The ring is free once every wave has left its last stage (every copy has landed).
   __syncthreads();
-  constexpr int XP = 32 * 32 * NRA * (PART ? 4 : 2);
+  constexpr int XP = 32 * 32 * NRA * (OUT == kOutPart ? 4 : 2);
   static_assert(C::NW * XP <= C::kLds, "LDS for the stores");
-  store_block<NRA, NCB, PART>(acc, p, nb, b0 + wb * NCB * 32, a0 + wa * NRA * 32, split, lane,
+  store_block<NRA, NCB, OUT>(acc, p, nb, b0 + wb * NCB * 32, a0 + wa * NRA * 32, split, lane,
                               smem + wave * XP);
 }
 
@@ -530,7 +538,7 @@ __device__ __forceinline__ void pp_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-template <bool TRB, bool PART>
+template <bool TRB, int OUT>
 __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
   constexpr int NRA = 4, NCB = 2, TILE = kPpTile, BOFF = 3 * TILE;
   __shared__ __attribute__((aligned(1024))) char smem[5 * TILE];
@@ -726,7 +734,7 @@ __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
   // No memory half reads the slots any more (group 0 passed the barrier closing the last one; group 1
   // reads none in its last compute half) and every copy has landed, so each wave stages its stores in its
   // own 16 KB of them.
-  store_block<NRA, NCB, PART>(acc, p, nb, b0 + 64 * wb, a0 + 128 * wa, split, lane, smem + wave * 16384);
+  store_block<NRA, NCB, OUT>(acc, p, nb, b0 + 64 * wb, a0 + 128 * wa, split, lane, smem + wave * 16384);
 }
 
 // Few rows: the other operand streams past once, non-temporally. 60 rows, d = 2560, K = 151,936:
@@ -737,50 +745,64 @@ using RingFew128 = RingCfg<256, 128, 4, 2, 3, 64, true>;
 // Narrow outputs, two workgroups to a CU.
 using RingNarrow = RingCfg<128, 128, 2, 2, 2>;
 using RingNarrow64 = RingCfg<128, 64, 2, 2, 3>;
-// Short sums: the stores bound the call, and three workgroups to a CU hide one another's loads and
-// stores (32768 x 4096 outputs of 256 terms 117 us with two of 64-deep stages, 104 with these).
-using RingShort = RingCfg<128, 128, 2, 2, 3, 32>;
+// Short sums: loads, stores and a few MFMAs a tile, which four workgroups to a CU hide from one another
+// (us, outputs of 32768 x 4096 and 151936 x 4096, 256 and 200 terms: two workgroups of 64-deep stages 117
+// and -, three with a third 32-deep slot 110 and 522, these 99 and 477; 256 x 128 tiles 101 and 498).
+using RingShort = RingCfg<128, 128, 2, 2, 2, 32>;
 
-template <class C, bool TRB, bool PART>
+template <class C, bool TRB, int OUT>
 hipError_t launch_ring(Prod p, hipStream_t stream) {
   const int64_t na = (p.na + C::BA - 1) / C::BA, nb = (p.nb + C::BB - 1) / C::BB;
   const int64_t n = na * nb * p.splits;
   if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
   p.n_btiles = static_cast<int>(nb);
-  hipLaunchKernelGGL((prod_ring_kernel<C, TRB, PART>), dim3(static_cast<unsigned>(n)),
+  hipLaunchKernelGGL((prod_ring_kernel<C, TRB, OUT>), dim3(static_cast<unsigned>(n)),
                      dim3(C::kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
-template <bool TRB, bool PART>
-hipError_t launch_prod(Prod p, hipStream_t stream) {
+template <bool TRB, int OUT>
+hipError_t launch_prod_out(Prod p, hipStream_t stream) {
   const ProdKind kind = prod_kind(TRB, p.na, p.nb, p.K);
   if (kind == kProdPp) {
     const int64_t na = (p.na + 255) / 256, nb = (p.nb + 255) / 256, n = na * nb * p.splits;
     if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
     p.n_btiles = static_cast<int>(nb);
-    hipLaunchKernelGGL((prod_pp_kernel<TRB, PART>), dim3(static_cast<unsigned>(n)), dim3(512), 0, stream,
+    hipLaunchKernelGGL((prod_pp_kernel<TRB, OUT>), dim3(static_cast<unsigned>(n)), dim3(512), 0, stream,
                        p);
     return hipGetLastError();
   }
   if constexpr (TRB) {
-    return launch_ring<RingShort, TRB, PART>(p, stream);
+    return launch_ring<RingShort, TRB, OUT>(p, stream);
   } else {
     if (kind == kProdFew)
-      return p.nb > 64 ? launch_ring<RingFew128, TRB, PART>(p, stream)
-                       : launch_ring<RingFew, TRB, PART>(p, stream);
-    return p.nb > 64 ? launch_ring<RingNarrow, TRB, PART>(p, stream)
-                     : launch_ring<RingNarrow64, TRB, PART>(p, stream);
+      return p.nb > 64 ? launch_ring<RingFew128, TRB, OUT>(p, stream)
+                       : launch_ring<RingFew, TRB, OUT>(p, stream);
+    return p.nb > 64 ? launch_ring<RingNarrow, TRB, OUT>(p, stream)
+                     : launch_ring<RingNarrow64, TRB, OUT>(p, stream);
   }
+}
+
+// fp32 sums of a product with one operand across the sum.
+hipError_t launch_prod_part(const Prod& p, hipStream_t stream) {
+  return launch_prod_out<false, kOutPart>(p, stream);
+}
+
+// The bf16 product of two operands across the sum. An output that would fill the 256 MB Infinity Cache is
+// written past it (151936 x 2560 outputs of 60 terms 174 ->
+// 141 us); a smaller one stays there for its next reader (50257 x 1000 outputs 34 us, 43 non-temporally).
+hipError_t launch_prod(const Prod& p, hipStream_t stream) {
+  return 2 * p.na * p.nb >= (int64_t(256) << 20) ? launch_prod_out<true, kOutStream>(p, stream)
+                                                : launch_prod_out<true, kOutKeep>(p, stream);
 }
 
 // ---------------------------------------------------------------------------------------
 // fp32 GEMM: out(a, b) = sum_k A(k, a) B(k, b) on v_mfma_f32_32x32x2_f32 (fp32 products and sums). Four
 // waves, 32-deep stages staged through registers. An operand is either [K, n] (TR) or [n, K] row-major;
-// any size and 4-byte alignment. ROWS = 128: 128 x 128 tile, waves of 128 a x 32 b. ROWS = 32, for up to
-// 32 rows: 128 x 32 tile, waves of 32 a (a 128-row tile would spend its MFMAs on rows that are not there:
-// 8 rows at d = 64, V = 256 11 us, of which 4 MFMAs).
-// Tile log-masses are of a wave's ids (128 or 32).
+// any size and 4-byte alignment. ROWS = 64: 128 x 64 tile, waves of 64 a x 32 b, three workgroups
+// to a CU. ROWS = 32, for up to 32 rows: 128 x 32 tile, waves of 32 a x 32 b. Measured: 128 x 128 tiles take
+// 11 us for 8 rows at d = 64, V = 256, 4 of them MFMAs on rows that are not there, these 5.6.
+// Tile log-masses are of a wave's ids (64 or 32).
 
 struct F32Args {
   const float* A;
@@ -806,11 +828,12 @@ struct F32Args {
 
 enum F32Epi : int { kF32Part = 0, kF32Out = 1, kF32Nll = 2, kF32Grad = 3 };
 
-// 32 x N values of an operand in LDS as [k][i] rows of N + 4, N / 8 a thread: TR along a row of K, else
-// along K; 0 past the ends.
+// 32 x N values of an operand in LDS as rows of k, column i at i ^ 32 (k % 2) (the two halves of a wave
+// read neighbouring k: other banks), N / 8 a thread: TR along a row of K, else along K; 0 past the ends.
 template <bool TR, int N>
 struct F32Stage {
-  static constexpr int VT = N / 8, LD = N + 4;
+  static constexpr int VT = N / 8, LD = N < 64 ? 64 : N;  // VT: 4, 8 or 16, which divide 32
+  static __device__ __forceinline__ int at(int k, int i) { return k * LD + (i ^ (32 * (k & 1))); }
   f32x4 r[VT / 4];
   __device__ __forceinline__ void load(const float* X, int64_t ld, int64_t i0, int64_t n, int64_t k0,
                                        int64_t ke) {
@@ -830,26 +853,27 @@ struct F32Stage {
   __device__ __forceinline__ void store(float* S) const {
     const int tid = threadIdx.x;
     if constexpr (TR) {
-      float* q = S + (tid / 8) * LD + VT * (tid % 8);
+      float* q = S + at(tid / 8, VT * (tid % 8));
 #pragma unroll
       for (int j = 0; j < VT / 4; ++j) *reinterpret_cast<f32x4*>(q + 4 * j) = r[j];
     } else {
 #pragma unroll
       for (int j = 0; j < VT; ++j)
-        S[(VT * (tid % (32 / VT)) + j) * LD + tid / (32 / VT)] = r[j / 4][j % 4];
+        S[at(VT * (tid % (32 / VT)) + j, tid / (32 / VT))] = r[j / 4][j % 4];
     }
   }
 };
 
 template <bool TRA, bool TRB, int EPI, int ROWS>
 __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
-  constexpr int BK = 32, NRA = ROWS == 128 ? 4 : 1, IDS = 32 * NRA;  // a of a wave
+  constexpr int BK = 32, NRA = ROWS / 32, IDS = 32 * NRA;  // a of a wave
+  static_assert(ROWS == 32 || ROWS == 64, "wave layouts");
   using SA = F32Stage<TRA, 128>;
   using SB = F32Stage<TRB, ROWS>;
   __shared__ __attribute__((aligned(16))) float As[2][BK * SA::LD], Bs[2][BK * SB::LD];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int half = lane >> 5;
-  const int wa = ROWS == 128 ? 0 : wave * 32, wb = ROWS == 128 ? wave * 32 : 0;
+  const int wa = ROWS == 64 ? (wave & 1) * 64 : wave * 32, wb = ROWS == 64 ? (wave >> 1) * 32 : 0;
   const int64_t K = p.count_k ? *p.count_k : p.K;
   const int64_t nb = p.count_b ? *p.count_b : p.nb;
   const int n_atiles = static_cast<int>((p.na + 127) / 128);
@@ -882,15 +906,16 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
         ra.load(p.A, p.lda, a0, p.na, k0 + BK, ke);
         rb.load(p.B, p.ldb, b0, nb, k0 + BK, ke);
       }
-      const float* sa = As[buf] + wa + (lane & 31);
-      const float* sb = Bs[buf] + wb + (lane & 31);
+      // k = kk + half with kk even: the permutation goes by the half.
+      const float* sa = As[buf] + half * SA::LD;
+      const float* sb = Bs[buf] + half * SB::LD + ((wb + (lane & 31)) ^ (32 * half));
 #pragma unroll
       for (int kk = 0; kk < BK; kk += 2) {
-        const float b = sb[(kk + half) * SB::LD];
+        const float b = sb[kk * SB::LD];
 #pragma unroll
         for (int i = 0; i < NRA; ++i)
-          acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(sa[(kk + half) * SA::LD + 32 * i], b, acc[i], 0,
-                                                        0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+              sa[kk * SA::LD + ((wa + 32 * i + (lane & 31)) ^ (32 * half))], b, acc[i], 0, 0, 0);
       }
       if (more) {
         ra.store(As[buf ^ 1]);
@@ -986,7 +1011,7 @@ template <bool TRA, bool TRB, int EPI>
 hipError_t launch_f32(const F32Args& p, hipStream_t stream) {
   if constexpr (!TRB)  // the products over the rows have the vocabulary there, many ids
     if (p.nb <= kF32FewRows) return launch_f32_rows<TRA, TRB, EPI, 32>(p, stream);
-  return launch_f32_rows<TRA, TRB, EPI, 128>(p, stream);
+  return launch_f32_rows<TRA, TRB, EPI, 64>(p, stream);
 }
 
 // ---------------------------------------------------------------------------------------
@@ -1037,57 +1062,58 @@ __global__ __launch_bounds__(64) void dh_finish_kernel(const NllArgs a, int64_t 
   }
 }
 
-// The expander's trunk gradient: the product's parts and the residual path's R branch gradients, in
-// fp32, rounded once. A wave takes 256 columns of a row.
-__global__ __launch_bounds__(64) void expand_dh_finish_kernel(const ExpandBackwardArgs a) {
-  const int64_t p = blockIdx.x;
+// The expander's trunk gradient (the product's parts and the residual path's R branch gradients, in fp32,
+// rounded once) and bias gradient, in one launch: the first n_dh workgroups take four blocks of 256 columns
+// of trunk rows, the others 64 features each.
+__global__ __launch_bounds__(256) void expand_finish_kernel(const ExpandBackwardArgs a, int64_t n_dh) {
   const int d = a.d, R = static_cast<int>(a.R);
-  const int j = blockIdx.y * 256 + 4 * threadIdx.x;
-  if (j >= d) return;
-  const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d + j;
-  f32x4 v = sum_parts(a.part + p * d + j, a.P * d, a.splits);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (blockIdx.x < n_dh) {
+    const int blocks = (d + 255) / 256;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + wave;
+    const int64_t p = at / blocks;
+    const int j = static_cast<int>(at % blocks) * 256 + 4 * lane;
+    if (p >= a.P || j >= d) return;
+    const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d + j;
+    f32x4 v = sum_parts(a.part + p * d + j, a.P * d, a.splits);
 #pragma unroll 8
-  for (int z = 0; z < R; ++z) {
-    const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d);
+    for (int z = 0; z < R; ++z) {
+      const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
+      for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
+    }
+    store4(static_cast<__bf16*>(a.dh) + p * d + j, v);
+    return;
   }
-  store4(static_cast<__bf16*>(a.dh) + p * d + j, v);
-}
-
-// dc: the sum over the trunk rows of every branch feature's gradient. A workgroup takes 128 features
-// (16 lanes of 8) with 64 rows side by side.
-__global__ __launch_bounds__(1024) void expand_dc_kernel(const __bf16* __restrict__ dout,
-                                                         __bf16* __restrict__ dc, int64_t P,
-                                                         int64_t n) {
-  __shared__ float part[16][129];
-  const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * 128 + 8 * c;
+  // dc: the sum over the trunk rows of every branch feature's gradient, 32 rows side by side.
+  __shared__ float part[4][65];
+  const int64_t n = a.R * d, j0 = (blockIdx.x - n_dh) * 64;
+  const int c = threadIdx.x & 7, r = threadIdx.x >> 3;
+  const int64_t j = j0 + 8 * c;
   float s[8] = {};
-  if (j < n)
-    for (int64_t p = r; p < P; p += 64) {
-      const bf16x8 v = *reinterpret_cast<const bf16x8*>(dout + p * n + j);
+  if (j < n) {
+    const __bf16* dout = static_cast<const __bf16*>(a.dout) + j;
+#pragma unroll 8
+    for (int64_t p = r; p < a.P; p += 32) {
+      const bf16x8 v = *reinterpret_cast<const bf16x8*>(dout + p * n);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += static_cast<float>(v[i]);
     }
-  // The four rows of a wave first, then the 16 waves.
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    s[i] += __shfl_xor(s[i], 16);
-    s[i] += __shfl_xor(s[i], 32);
   }
-  if ((threadIdx.x & 63) < 16) {
+  // The eight rows of a wave first, then the four waves.
 #pragma unroll
-    for (int i = 0; i < 8; ++i) part[threadIdx.x >> 6][8 * c + i] = s[i];
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int o = 8; o < 64; o <<= 1) s[i] += __shfl_xor(s[i], o);
+  if (lane < 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) part[wave][8 * c + i] = s[i];
   }
   __syncthreads();
-  if (threadIdx.x < 128) {
-    float t = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) t += part[i][threadIdx.x];
-    const int64_t o = static_cast<int64_t>(blockIdx.x) * 128 + threadIdx.x;
-    if (o < n) dc[o] = static_cast<__bf16>(t);
-  }
+  if (threadIdx.x < 64 && j0 + threadIdx.x < n)
+    static_cast<__bf16*>(a.dc)[j0 + threadIdx.x] =
+        static_cast<__bf16>((part[0][threadIdx.x] + part[1][threadIdx.x]) +
+                            (part[2][threadIdx.x] + part[3][threadIdx.x]));
 }
 
 }  // namespace
@@ -1166,7 +1192,7 @@ hipError_t launch_nll_backward(const NllArgs& a, hipStream_t stream) {
       p.part_stride = part_stride;
       p.accumulate = v0 > 0;
       p.splits = a.splits;
-      e = launch_prod<false, true>(p, stream);
+      e = launch_prod_part(p, stream);
       if (e != hipSuccess) return e;
       }
       if (a.dw) {
@@ -1180,7 +1206,7 @@ hipError_t launch_nll_backward(const NllArgs& a, hipStream_t stream) {
         q.count = M > 0 ? a.count : nullptr;
         q.out = static_cast<__bf16*>(a.dw) + v0 * a.d;
         q.splits = 1;
-        e = launch_prod<true, false>(q, stream);
+        e = launch_prod(q, stream);
       }
     } else {
       const float* w = static_cast<const float*>(a.w) + v0 * a.d;
@@ -1253,12 +1279,7 @@ hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t strea
     p.part = a.part;
     p.part_stride = a.P * a.d;
     p.splits = a.splits;
-    e = launch_prod<false, true>(p, stream);
-    if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(expand_dh_finish_kernel,
-                       dim3(static_cast<unsigned>(a.P), static_cast<unsigned>((a.d + 255) / 256)),
-                       dim3(64), 0, stream, a);
-    e = hipGetLastError();
+    e = launch_prod_part(p, stream);
     if (e != hipSuccess) return e;
   }
   if (a.dW) {
@@ -1271,15 +1292,16 @@ hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t strea
     q.K = a.P;
     q.out = static_cast<__bf16*>(a.dW);
     q.splits = 1;
-    e = launch_prod<true, false>(q, stream);
+    e = launch_prod(q, stream);
     if (e != hipSuccess) return e;
   }
-  if (a.dc) {
-    hipLaunchKernelGGL(expand_dc_kernel, dim3(static_cast<unsigned>((n + 127) / 128)), dim3(1024), 0,
-                       stream, static_cast<const __bf16*>(a.dout), static_cast<__bf16*>(a.dc), a.P, n);
-    e = hipGetLastError();
-  }
-  return e;
+  const int64_t n_dh = a.dh ? (a.P * ((a.d + 255) / 256) + 3) / 4 : 0;
+  const int64_t blocks = n_dh + (a.dc ? (n + 63) / 64 : 0);
+  if (blocks == 0) return hipSuccess;
+  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL(expand_finish_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a,
+                     n_dh);
+  return hipGetLastError();
 }
 
 }  // namespace dbl
