@@ -828,38 +828,62 @@ struct F32Args {
 
 enum F32Epi : int { kF32Part = 0, kF32Out = 1, kF32Nll = 2, kF32Grad = 3 };
 
-// 32 x N values of an operand in LDS as rows of k, column i at i ^ 32 (k % 2) (the two halves of a wave
-// read neighbouring k: other banks), N / 8 a thread: TR along a row of K, else along K; 0 past the ends.
+// 32 x N values of an operand in LDS as rows of k, N / 32 groups of four a thread: eight lanes read 128
+// contiguous bytes (of a row of K with TR, else along K; with 64 bytes a thread the vector cache's lines
+// were touched four times). Column i of row k lies at i ^ perm(k): the halves of a wave read neighbouring
+// k from other banks, and the eight lanes of an operand along K write theirs to other banks. The loads are
+// buffer loads, which give 0 past the array's end, so that none of them has a condition (with one, the two
+// paths' loads met in the same registers and each stage waited for its loads before its MFMAs: 120 us for
+// 512 x 500 against 20,000 ids): TR past the last row (values past a row's end belong to the next one, and
+// to outputs that do not exist), else with the rows past the last one repeating it and the values past K
+// set to 0 as they are stored.
 template <bool TR, int N>
 struct F32Stage {
-  static constexpr int VT = N / 8, LD = N < 64 ? 64 : N;  // VT: 4, 8 or 16, which divide 32
-  static __device__ __forceinline__ int at(int k, int i) { return k * LD + (i ^ (32 * (k & 1))); }
-  f32x4 r[VT / 4];
-  __device__ __forceinline__ void load(const float* X, int64_t ld, int64_t i0, int64_t n, int64_t k0,
-                                       int64_t ke) {
-    const int tid = threadIdx.x;
-    const int64_t row = TR ? k0 + tid / 8 : i0 + tid / (32 / VT);
-    const int64_t col = TR ? i0 + VT * (tid % 8) : k0 + VT * (tid % (32 / VT));
-    const int64_t left = row < (TR ? ke : n) ? (TR ? n : ke) - col : 0;
-    const float* q = X + row * ld + col;
-    if (left >= VT) {
+  static constexpr int G = N / 32, LD = N < 64 ? 64 : N;
+  static __device__ __forceinline__ int perm(int k) { return 8 * ((k >> 2) & 7) ^ 32 * (k & 1); }
+  static __device__ __forceinline__ int at(int k, int i) { return k * LD + (i ^ perm(k)); }
+  f32x4 r[G];
+  uint32_t off[G];  // of a group in the tile, bytes
+  __device__ __forceinline__ void init(int64_t ld, int64_t i0, int64_t n) {
+    const int t8 = threadIdx.x >> 3, c4 = 4 * (threadIdx.x & 7);
 #pragma unroll
-      for (int j = 0; j < VT / 4; ++j) r[j] = *reinterpret_cast<const f32x4u*>(q + 4 * j);
-    } else {
-#pragma unroll
-      for (int j = 0; j < VT; ++j) r[j / 4][j % 4] = j < left ? q[j] : 0.0f;
+    for (int j = 0; j < G; ++j) {
+      if constexpr (TR) {
+        off[j] = static_cast<uint32_t>(4 * (t8 * ld + c4 + 32 * j));
+      } else {
+        const int row = t8 + 32 * j;
+        off[j] = static_cast<uint32_t>(4 * ((row < n - i0 ? row : n - i0 - 1) * ld + c4));
+      }
     }
   }
-  __device__ __forceinline__ void store(float* S) const {
-    const int tid = threadIdx.x;
+  // rows: of the array (K for TR, n else).
+  __device__ __forceinline__ void load(const float* X, int64_t ld, int64_t i0, int64_t k0, int64_t rows) {
+    const int64_t from = TR ? k0 * ld + i0 : i0 * ld + k0;
+    const int64_t left = 4 * (rows * ld - from);
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<float*>(X + from), 0,
+        static_cast<int>(left < 0xffffffffll ? static_cast<uint32_t>(left) : 0xffffffffu), 0x00027000);
+#pragma unroll
+    for (int j = 0; j < G; ++j)
+      r[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[j], 0, 0));
+  }
+  // left: k of the stage that are there.
+  __device__ __forceinline__ void store(float* S, int64_t left) {
+    const int t8 = threadIdx.x >> 3, c4 = 4 * (threadIdx.x & 7);
     if constexpr (TR) {
-      float* q = S + at(tid / 8, VT * (tid % 8));
 #pragma unroll
-      for (int j = 0; j < VT / 4; ++j) *reinterpret_cast<f32x4*>(q + 4 * j) = r[j];
+      for (int j = 0; j < G; ++j) *reinterpret_cast<f32x4*>(S + at(t8, c4 + 32 * j)) = r[j];
     } else {
+      if (left < 32) {
 #pragma unroll
-      for (int j = 0; j < VT; ++j)
-        S[at(VT * (tid % (32 / VT)) + j, tid / (32 / VT))] = r[j / 4][j % 4];
+        for (int j = 0; j < G; ++j)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) r[j][q] = c4 + q < left ? r[j][q] : 0.0f;
+      }
+#pragma unroll
+      for (int j = 0; j < G; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) S[at(c4 + q, t8 + 32 * j)] = r[j][q];
     }
   }
 };
@@ -878,8 +902,11 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
   const int64_t nb = p.count_b ? *p.count_b : p.nb;
   const int n_atiles = static_cast<int>((p.na + 127) / 128);
   const int bt = blockIdx.x % p.n_btiles, rest = blockIdx.x / p.n_btiles;
-  const int at = rest % n_atiles, split = rest / n_atiles;
-  const int64_t a0 = static_cast<int64_t>(at) * 128, b0 = static_cast<int64_t>(bt) * ROWS;
+  // In scalar registers: the loads' resources are made of these.
+  const int at = __builtin_amdgcn_readfirstlane(rest % n_atiles);
+  const int split = __builtin_amdgcn_readfirstlane(rest / n_atiles);
+  const int64_t a0 = static_cast<int64_t>(at) * 128;
+  const int64_t b0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(bt)) * ROWS;
   if (b0 >= nb) return;
   const int64_t per = ((K + p.splits - 1) / p.splits + BK - 1) / BK * BK;
   const int64_t kb = split * per < K ? split * per : K;
@@ -894,33 +921,35 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
   if (kb < ke) {
     SA ra;
     SB rb;
-    ra.load(p.A, p.lda, a0, p.na, kb, ke);
-    rb.load(p.B, p.ldb, b0, nb, kb, ke);
-    ra.store(As[0]);
-    rb.store(Bs[0]);
+    ra.init(p.lda, a0, p.na);
+    rb.init(p.ldb, b0, nb);
+    auto load = [&](int64_t k0) {
+      ra.load(p.A, p.lda, a0, k0, TRA ? K : p.na);
+      rb.load(p.B, p.ldb, b0, k0, TRB ? K : nb);
+    };
+    auto store = [&](int buf, int64_t k0) {
+      ra.store(As[buf], ke - k0);
+      rb.store(Bs[buf], ke - k0);
+    };
+    load(kb);
+    store(0, kb);
     __syncthreads();
     int buf = 0;
     for (int64_t k0 = kb; k0 < ke; k0 += BK, buf ^= 1) {
       const bool more = k0 + BK < ke;
-      if (more) {
-        ra.load(p.A, p.lda, a0, p.na, k0 + BK, ke);
-        rb.load(p.B, p.ldb, b0, nb, k0 + BK, ke);
-      }
-      // k = kk + half with kk even: the permutation goes by the half.
+      if (more) load(k0 + BK);
       const float* sa = As[buf] + half * SA::LD;
-      const float* sb = Bs[buf] + half * SB::LD + ((wb + (lane & 31)) ^ (32 * half));
+      const float* sb = Bs[buf] + half * SB::LD;
 #pragma unroll
-      for (int kk = 0; kk < BK; kk += 2) {
-        const float b = sb[kk * SB::LD];
+      for (int kk = 0; kk < BK; kk += 2) {  // k = kk + half, kk even
+        const int x = SA::perm(kk) ^ (32 * half);
+        const float b = sb[kk * SB::LD + ((wb + (lane & 31)) ^ x)];
 #pragma unroll
         for (int i = 0; i < NRA; ++i)
           acc[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-              sa[kk * SA::LD + ((wa + 32 * i + (lane & 31)) ^ (32 * half))], b, acc[i], 0, 0, 0);
+              sa[kk * SA::LD + ((wa + 32 * i + (lane & 31)) ^ x)], b, acc[i], 0, 0, 0);
       }
-      if (more) {
-        ra.store(As[buf ^ 1]);
-        rb.store(Bs[buf ^ 1]);
-      }
+      if (more) store(buf ^ 1, k0 + BK);
       __syncthreads();
     }
   }
