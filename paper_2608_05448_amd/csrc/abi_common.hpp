@@ -114,7 +114,7 @@ inline WsLayout layout(int op, const dbl_shape& s) {
       sizes[3] = B * K * R * static_cast<size_t>(s.d) * sizeof(float);
       n = 6;
       if (op == DBL_OP_HEAD_NLL) {
-        sizes[4] = B * K * R * dbl::nll_tiles(false, s.B * s.K * s.R, s.V) * sizeof(float);
+        sizes[4] = B * K * R * dbl::nll_tiles(false, s.V) * sizeof(float);
         sizes[5] = B * K * R * sizeof(float);
       } else {
         const int64_t M = s.B * s.K * s.R;

@@ -95,10 +95,11 @@ dbl_status check_tensors(int64_t n, const void* const* grads, const int64_t* num
 
 // No C++ exception (a host allocation that fails) crosses the C boundary.
 template <class F>
-dbl_status guarded(F f) {
+dbl_status guarded(F f) noexcept {
   try {
     return f();
-  } catch (const std::bad_alloc&) {
+  } catch (...) {
+    g_last_error.clear();
     return DBL_EHIP;
   }
 }
@@ -109,20 +110,22 @@ extern "C" {
 
 dbl_status dbl_head_nll(dbl_shape s, int dt, const void* h, const void* w, const int32_t* x,
                         float* nll, float* lse, void* ws, size_t ws_bytes, void* stream) {
-  if (dbl_status st = check_nll(s, dt)) return st;
-  if (!w || (s.B > 0 && (!h || !x || !nll || !lse))) return fail(DBL_EINVAL, "NULL pointer");
-  if (dbl_status st = check_aligned({{h, "h"}, {w, "w"}, {x, "x"}, {nll, "nll"}, {lse, "lse"}}))
-    return st;
-  if (s.B == 0) return ok();
-  WsLayout L;
-  if (dbl_status st = check_ws(DBL_OP_HEAD_NLL, s, ws, ws_bytes, &L)) return st;
-  char* const base = static_cast<char*>(ws);
-  dbl::NllArgs a = nll_args(s, dt, h, w, x, base, L);
-  a.nll = nll;
-  a.lse = lse;
-  a.lmass = reinterpret_cast<float*>(base + L.off[4]);
-  a.tgt = reinterpret_cast<float*>(base + L.off[5]);
-  return hip_status(dbl::launch_nll(a, static_cast<hipStream_t>(stream)), "head nll launch");
+  return guarded([&]() -> dbl_status {
+    if (dbl_status st = check_nll(s, dt)) return st;
+    if (!w || (s.B > 0 && (!h || !x || !nll || !lse))) return fail(DBL_EINVAL, "NULL pointer");
+    if (dbl_status st = check_aligned({{h, "h"}, {w, "w"}, {x, "x"}, {nll, "nll"}, {lse, "lse"}}))
+      return st;
+    if (s.B == 0) return ok();
+    WsLayout L;
+    if (dbl_status st = check_ws(DBL_OP_HEAD_NLL, s, ws, ws_bytes, &L)) return st;
+    char* const base = static_cast<char*>(ws);
+    dbl::NllArgs a = nll_args(s, dt, h, w, x, base, L);
+    a.nll = nll;
+    a.lse = lse;
+    a.lmass = reinterpret_cast<float*>(base + L.off[4]);
+    a.tgt = reinterpret_cast<float*>(base + L.off[5]);
+    return hip_status(dbl::launch_nll(a, static_cast<hipStream_t>(stream)), "head nll launch");
+  });
 }
 
 dbl_status dbl_head_nll_backward(dbl_shape s, int dt, const void* h, const void* w,

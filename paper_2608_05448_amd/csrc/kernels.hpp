@@ -265,13 +265,10 @@ inline int grad_splits(int64_t na, int64_t nb, int64_t K) {
   return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
 }
 
-// Rows up to which the fp32 kernel takes tiles of 32 rows, and the tile log-masses a row has: of 128 ids,
-// in fp32 of 64, and of 32 in that kernel.
+// Rows up to which the fp32 kernel takes tiles of 32 rows.
 constexpr int64_t kF32FewRows = 32;
-inline int64_t nll_tiles(bool bf16, int64_t M, int64_t V) {
-  const int64_t ids = bf16 ? kTile : M <= kF32FewRows ? 32 : 64;
-  return (V + ids - 1) / ids;
-}
+// Tile log-masses of a row: of 128 ids, in fp32 of 32.
+inline int64_t nll_tiles(bool bf16, int64_t V) { return bf16 ? (V + kTile - 1) / kTile : (V + 31) / 32; }
 
 // The splits for fp32, whose kernel has 128 x 64 tiles and 32-deep stages: small problems are bound by the
 // walk over K (a stage takes about 2 us to load), so parts have 32 terms at least.

@@ -802,7 +802,7 @@ hipError_t launch_prod(const Prod& p, hipStream_t stream) {
 // any size and 4-byte alignment. ROWS = 64: 128 x 64 tile, waves of 64 a x 32 b, three workgroups
 // to a CU. ROWS = 32, for up to 32 rows: 128 x 32 tile, waves of 32 a x 32 b. Measured: 128 x 128 tiles take
 // 11 us for 8 rows at d = 64, V = 256, 4 of them MFMAs on rows that are not there, these 5.6.
-// Tile log-masses are of a wave's ids (64 or 32).
+// Tile log-masses are of 32 ids in both, so that a row's sums do not depend on the kernel.
 
 struct F32Args {
   const float* A;
@@ -982,27 +982,29 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
     if (aw >= p.na) return;
     const int lim = static_cast<int>(p.na - aw < IDS ? p.na - aw : IDS) - 4 * half;
     if constexpr (EPI == kF32Nll) {
-      float x[16 * NRA];
-#pragma unroll
-      for (int i = 0; i < 16 * NRA; ++i)
-        x[i] = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) < lim ? acc[i >> 4][i & 15] : -INFINITY;
       const int64_t o = b < nb ? p.rows[b].token - aw - 4 * half : -1;
-      if (o >= 0 && o < lim && !(o & 4)) {
-        float t = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 16 * NRA; ++i)
-          t = o == 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) ? x[i] : t;
-        p.tgt[b] = t;
+      for (int i = 0; i < NRA; ++i) {
+        if (aw + 32 * i >= p.na) break;
+        float x[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = 32 * i + 8 * (r >> 2) + (r & 3) < lim ? acc[i][r] : -INFINITY;
+        if (o >= 32 * i && o < 32 * i + 32 && o < lim && !(o & 4)) {
+          float t = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) t = o == 32 * i + 8 * (r >> 2) + (r & 3) ? x[r] : t;
+          p.tgt[b] = t;
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[r]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        float s = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += __expf(x[r] - mx);
+        s += __shfl_xor(s, 32);
+        if (b < nb && half == 0) p.lmass[b * p.nT + aw / 32 + i] = mx + logf(s);
       }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 16 * NRA; ++i) mx = fmaxf(mx, x[i]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      float s = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 16 * NRA; ++i) s += __expf(x[i] - mx);
-      s += __shfl_xor(s, 32);
-      if (b < nb && half == 0) p.lmass[b * p.nT + aw / IDS] = mx + logf(s);
     } else {
       if (b >= nb) return;
       const TrainRow row = p.rows[b];
@@ -1149,7 +1151,7 @@ __global__ __launch_bounds__(256) void expand_finish_kernel(const ExpandBackward
 
 hipError_t launch_nll(const NllArgs& a, hipStream_t stream) {
   const int64_t M = a.P * a.R;
-  const int nT = static_cast<int>(nll_tiles(a.bf16, M, a.V));
+  const int nT = static_cast<int>(nll_tiles(a.bf16, a.V));
   hipError_t e = gather_rows(a, stream);
   if (e != hipSuccess) return e;
   if (a.bf16) {

@@ -144,6 +144,15 @@ HEAD_CASES = [
     ("bf16", 5, 13, 5, 72, 1153, "some"),
     ("bf16", 2, 4, 2, 64, 300, "all"),
     ("bf16", 1, 70, 1, 2048, 9000, "some"),     # sums that start further on
+    ("bf16", 1, 33, 1, 104, 513, "some"),       # a partial last stage: 64-row tiles, 128-row tiles,
+    ("bf16", 2, 40, 1, 1000, 901, "some"),      # 256-row tiles, and a hidden size below one stage
+    ("bf16", 6, 40, 1, 136, 901, "some"),
+    ("bf16", 2, 70, 2, 8, 2100, "some"),
+    ("bf16", 3, 100, 1, 192, 600, "some"),      # 300 rows: the products' 256 x 256 tiles, short sums
+    ("bf16", 11, 50, 1, 264, 3000, "some"),     # both products on 256 x 256 tiles, partial last stages
+    ("bf16", 5, 100, 1, 72, 2500, "none"),      # a narrow hidden size: 128-column tiles
+    ("fp32", 1, 31, 1, 63, 95, "none"), ("fp32", 1, 33, 1, 65, 97, "none"),
+    ("fp32", 2, 64, 3, 250, 3001, "some"),      # sums in several parts
 ]
 
 
@@ -224,12 +233,13 @@ def test_pieces_of_the_vocabulary():
 
 def test_rows_do_not_depend_on_the_batch():
     from paper_2608_05448_amd import dblast as D
-    for d, R in ((64, 3), (2048, 2)):
-        h, w, x, g = [t.cuda() for t in _inputs("bf16", 40, 5, R, d, 5000, seed=9, mask="some")]
+    for dtype, d, R in (("bf16", 64, 3), ("bf16", 2048, 2), ("bf16", 200, 3), ("bf16", 96, 2),
+                        ("fp32", 40, 3)):
+        h, w, x, g = [t.cuda() for t in _inputs(dtype, 40, 5, R, d, 5000, seed=9, mask="some")]
         nll, lse = D.dbl_head_nll(h, w, x)
         for b, n in ((0, 1), (3, 8), (20, 20)):
             a, c = D.dbl_head_nll(h[b:b + n].clone(), w, x[b:b + n].clone())
-            assert torch.equal(a, nll[b:b + n]) and torch.equal(c, lse[b:b + n]), (d, b, n)
+            assert torch.equal(a, nll[b:b + n]) and torch.equal(c, lse[b:b + n]), (dtype, d, b, n)
 
 
 def test_more_positions_than_are_counted_inline():
@@ -269,6 +279,7 @@ EXPAND_CASES = [
     # B, K, R, d
     (1, 1, 1, 32), (1, 1, 3, 64), (1, 15, 4, 96), (2, 7, 5, 160), (3, 50, 2, 128), (5, 13, 8, 256),
     (1, 63, 2, 64), (1, 64, 2, 64), (1, 65, 2, 64), (4, 16, 64, 32), (17, 16, 3, 288), (2, 200, 2, 512),
+    (5, 129, 2, 320), (9, 100, 4, 544), (1, 128, 5, 256),
 ]
 
 
