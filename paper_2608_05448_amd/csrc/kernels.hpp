@@ -232,11 +232,16 @@ inline int64_t nll_piece(int64_t M, int64_t V, int elem) {
 }
 
 // The kernel of a bf16 product [nb, na] over K terms (both: both operands lie across the sum): 256 x 256
-// tiles, one workgroup to a CU; 256-column tiles of up to 128 rows, one to a CU; smaller tiles.
-enum ProdKind : int { kProdPp = 0, kProdFew = 1, kProdSmall = 2 };
+// tiles, one workgroup to a CU; 256-column tiles of up to 128 rows, one to a CU; smaller tiles; for short
+// sums with both operands across them, a stream over the output. The last against the smaller tiles, us
+// (terms x output columns x rows): 200 x 4096 x 151936 317 and 477, 128 x 4096 x 151936 213 and 246, 256 x
+// 4096 x 32768 72 and 96, 100 x 2048 x 50000 38 and 50; but 168 x 1000 x 50257 34 and 31, 250 x 1024 x
+// 20000 25 and 20, 60 x 2560 x 151936 125 and 128, 30 x 2048 x 151936 118 and 107.
+enum ProdKind : int { kProdPp = 0, kProdFew = 1, kProdSmall = 2, kProdStream = 3 };
 inline ProdKind prod_kind(bool both, int64_t na, int64_t nb, int64_t K) {
   if (na > 128 && nb > 128 && K >= 512) return kProdPp;
-  return !both && na > 128 && nb <= 128 ? kProdFew : kProdSmall;
+  if (!both) return na > 128 && nb <= 128 ? kProdFew : kProdSmall;
+  return K > 64 && K <= 256 && na > 256 && na * nb >= (int64_t(1) << 26) ? kProdStream : kProdSmall;
 }
 
 // How many parts the sum over K of an [nb, na] product is split into (one operand across the sum).

@@ -430,8 +430,8 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
       reinterpret_cast<const char*>(p.B) + (TRB ? 0 : static_cast<int64_t>(2) * b0 * p.ldb);
   const uint32_t lds0 = lds_addr(smem);
   const uint32_t lda2 = static_cast<uint32_t>(2 * p.lda), ldb2 = static_cast<uint32_t>(2 * p.ldb);
-  // Stage s: rows (or chunks) past the end of the range repeat its last one; what they hold meets
-  // zeros (see tail below).
+  // Stage s: rows (or chunks) past the end of the range repeat its last one; what they hold counts
+  // as 0 (see tail below).
   auto copy = [&](int s, int slot) {
     const int64_t k0 = kb + step * static_cast<int64_t>(s);
     const int left = static_cast<int>(K - k0 < BK ? K - k0 : BK);  // >= 1
@@ -487,7 +487,13 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void prod_ring_kernel(
           const int r = (wb * NCB + j) * 32 + (lane & 31);
           bf[j] = *reinterpret_cast<const bf16x8*>(sb + r * 128 + ((2 * ks + half) ^ row_swz(r)) * 16);
         }
-        if (tail) bf[j] = keep_first(bf[j], left - 16 * ks - 8 * half);
+      }
+      if (tail) {  // both operands: what a copy past the end repeats may hold infinities
+        const int n = left - 16 * ks - 8 * half;
+#pragma unroll
+        for (int i = 0; i < NRA; ++i) af[i] = keep_first(af[i], n);
+#pragma unroll
+        for (int j = 0; j < NCB; ++j) bf[j] = keep_first(bf[j], n);
       }
 #pragma unroll
       for (int i = 0; i < NRA; ++i)
@@ -590,7 +596,7 @@ __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
                             (TRB ? kb * ldb2 : static_cast<int64_t>(2) * (b0 * p.ldb + kb));
   const uint32_t lds0 = lds_addr(smem) + wave * 4096;
   // The last stage of a range may hold fewer than 64 k: rows (or chunks) past them repeat the last row
-  // (the first chunk) and meet zeros in the B fragments.
+  // (the first chunk) and count as 0 in the fragments.
   const int last = static_cast<int>(ke - kb - 64 * static_cast<int64_t>(nk - 1));
   auto copy_A = [&](int s, int slot) {
     const char* base = baseA + static_cast<int64_t>(s) * 64 * lda2;
@@ -666,12 +672,15 @@ __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
         }
       }
     }
-    if (left < 64) {
+    if (left < 64) {  // both operands: what a copy past the end repeats may hold infinities
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
+      for (int ks = 0; ks < 2; ++ks) {
+        const int n = left - 16 * (kk0 + ks) - 8 * half;
 #pragma unroll
-        for (int j = 0; j < NCB; ++j)
-          bf[ks][j] = keep_first(bf[ks][j], left - 16 * (kk0 + ks) - 8 * half);
+        for (int i = 0; i < NRA; ++i) af[ks][i] = keep_first(af[ks][i], n);
+#pragma unroll
+        for (int j = 0; j < NCB; ++j) bf[ks][j] = keep_first(bf[ks][j], n);
+      }
     }
   };
   auto compute = [&]() {
@@ -761,6 +770,199 @@ hipError_t launch_ring(Prod p, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// Sums of 65 to 256 terms with both operands across the sum and a large output (the weight gradients of a
+// few blocks): the output is much larger than what it is made of, so the kernel is a stream of stores with
+// a few MFMAs between them. A workgroup of eight waves owns 512 columns of A, whose fragments for all K
+// (64 KT at most) stay in registers, 64 columns a wave, and walks a range of B's columns 64 at a time: a
+// [K, 64] tile per step, copied global -> LDS two steps ahead, one barrier a step. A's panel is read once
+// per range and B once per panel. prod_kind says where it is the faster form.
+// The stores are buffer stores, dropped by the hardware past the output's end, so that every step issues
+// the same number of them and the wait for a tile can leave the stores since its copy in flight: memory
+// operations of a wave complete in order.
+constexpr int kStreamTile = 64, kStreamPanel = 512;
+template <int KT, int OUT>
+__global__ __launch_bounds__(512, 2) void prod_stream_kernel(const Prod p, int per_range) {
+  constexpr int STAGE = KT * 8192, S = 3;         // bytes of a B tile: 64 KT rows of 128
+  constexpr int PER = STAGE / 1024 / 8;           // copies per wave and step
+  constexpr int NST = 8;                          // stores per wave and step
+  constexpr int RING = S * STAGE;
+  constexpr int AT = 2;                           // 64-row tiles of A's panel that pass through LDS at a time
+  constexpr int LDS = RING + 8 * 4096 > AT * 65536 ? RING + 8 * 4096 : AT * 65536;
+  static_assert(LDS <= 160 * 1024 && KT % AT == 0 && PER + 2 * NST <= 63, "LDS, vmcnt");
+  __shared__ __attribute__((aligned(1024))) char smem[LDS];
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t K = p.count ? *p.count : p.K;
+  // Panels of one range of B are consecutive, so that they share B's tiles in an XCD's L2.
+  const int n_panels = static_cast<int>((p.na + kStreamPanel - 1) / kStreamPanel);
+  const int L = xcd_remap(blockIdx.x, gridDim.x);
+  const int panel = __builtin_amdgcn_readfirstlane(L % n_panels);
+  const int range = __builtin_amdgcn_readfirstlane(L / n_panels);
+  const int64_t a0 = static_cast<int64_t>(panel) * kStreamPanel;
+  const int64_t tiles = (p.nb + kStreamTile - 1) / kStreamTile;
+  const int64_t t0 = static_cast<int64_t>(range) * per_range;
+  const int nt = static_cast<int>(tiles - t0 < per_range ? tiles - t0 : per_range);
+  if (nt <= 0) return;
+  const uint32_t lds0 = lds_addr(smem);
+  const int i16 = lane & 15, half = lane >> 5;
+
+  // A's fragments: 128 rows of the panel at a time through LDS (1 KB rows, one copy instruction each,
+  // chunk c of row k at c ^ tr_swz(k)); rows past K repeat the last one, and count as 0 (in both operands:
+  // what is repeated may hold infinities).
+  bf16x8 af[4 * KT][2];
+#pragma unroll
+  for (int kt = 0; kt < KT; kt += AT) {
+    if (64 * kt < K) {
+#pragma unroll
+      for (int i = 0; i < 8 * AT; ++i) {
+        const int r = 8 * AT * wave + i;
+        const int64_t k = 64 * kt + r < K ? 64 * kt + r : K - 1;
+        const int64_t c = a0 + 8 * (lane ^ tr_swz<512>(r));
+        lds_dma16(reinterpret_cast<const char*>(p.A) + 2 * k * p.lda,
+                  static_cast<uint32_t>(2 * (c < p.na ? c : p.na - 8)), lds0 + r * 1024);
+      }
+      wait_vmcnt<0>();
+      __syncthreads();
+    }
+#pragma unroll
+    for (int ks = 0; ks < 4 * AT; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        af[4 * kt + ks][i] = bf16x8{};
+        if (64 * kt + 16 * ks < K) {
+          const int k = 16 * ks + 8 * half + (i16 >> 2);
+          const int chunk = (4 * (2 * wave + i) + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ tr_swz<512>(k);
+          const char* q = smem + k * 1024 + chunk * 16 + (i16 & 1) * 8;
+          af[4 * kt + ks][i] = keep_first(join(lds_read_tr(q), lds_read_tr(q + 4096)),
+                                          static_cast<int>(K - 64 * kt) - 16 * ks - 8 * half);
+        }
+      }
+    __syncthreads();
+  }
+
+  // B tiles: row k of 64 columns at 128 k, chunk c at c ^ tr_swz(k); a copy instruction covers 8 rows.
+  uint32_t off[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = (wave * PER + i) * 8 + (lane >> 3);
+    const int64_t k = r < K ? r : K - 1;
+    off[i] = static_cast<uint32_t>(2 * k * p.ldb + 16 * ((lane & 7) ^ tr_swz<64>(r)));
+  }
+  auto copy = [&](int t) {
+    if (t >= nt || K == 0) return;
+    const int64_t at = t0 + t;
+    const char* base = reinterpret_cast<const char*>(p.B) + 2 * kStreamTile * at;
+    // The last tile may reach past B's columns: its chunks there are moved back onto the row's last one.
+    const int64_t left = p.ldb - kStreamTile * at;  // >= 8
+    const uint32_t to = lds0 + (t % S) * STAGE;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      uint32_t o = off[i];
+      if (left < kStreamTile) {
+        const int c = (lane & 7) ^ tr_swz<64>((wave * PER + i) * 8 + (lane >> 3));
+        if (8 * c >= left) o -= 16u * static_cast<uint32_t>(c - (left / 8 - 1));
+      }
+      lds_dma16(base, o, to + (wave * PER + i) * 1024);
+    }
+  };
+  copy(0);
+  copy(1);
+  char* const xp = smem + RING + wave * 4096;
+  const int64_t aw = a0 + 64 * wave;
+  for (int t = 0; t < nt; ++t) {
+    // Issued since step t's copies, two steps ago: two steps' stores and, but for the last step, one step's
+    // copies.
+    if (t + 1 < nt) {
+      if (t == 0) wait_vmcnt<PER>();
+      else if (t == 1) wait_vmcnt<PER + NST>();
+      else wait_vmcnt<PER + 2 * NST>();
+    } else {
+      if (t == 0) wait_vmcnt<0>();
+      else if (t == 1) wait_vmcnt<NST>();
+      else wait_vmcnt<2 * NST>();
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    copy(t + 2);  // into the slot of step t - 1, which every wave has read
+    const char* sb = smem + (t % S) * STAGE;
+    f32x16 acc[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < 4 * KT; ++ks) {
+      if (16 * ks < K) {
+        bf16x8 bf[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int k = 16 * ks + 8 * half + (i16 >> 2);
+          const int chunk = (4 * j + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1)) ^ tr_swz<64>(k);
+          const char* q = sb + k * 128 + chunk * 16 + (i16 & 1) * 8;
+          bf[j] = join(lds_read_tr(q), lds_read_tr(q + 512));
+        }
+        if (16 * ks + 16 > K) {
+#pragma unroll
+          for (int j = 0; j < 2; ++j) bf[j] = keep_first(bf[j], static_cast<int>(K) - 16 * ks - 8 * half);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks][i], bf[j], acc[i][j], 0, 0, 0);
+      }
+    }
+    // 32 rows x 64 columns at a time through LDS (chunk c of row r at c ^ (r % 8)): a store writes eight
+    // 128-byte row segments.
+    const int64_t b0 = kStreamTile * (t0 + t);
+    const int64_t rows = p.nb - b0 < kStreamTile ? p.nb - b0 : kStreamTile;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(p.out + b0 * p.na, 0,
+                                                        static_cast<int>(2 * rows * p.na), 0x00027000);
+    const int lr = lane & 31;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x16& v = acc[i][j];
+          *reinterpret_cast<bf16x4*>(xp + lr * 128 + ((4 * i + g) ^ (lr & 7)) * 16 + half * 8) =
+              bf16x4{static_cast<__bf16>(v[4 * g]), static_cast<__bf16>(v[4 * g + 1]),
+                     static_cast<__bf16>(v[4 * g + 2]), static_cast<__bf16>(v[4 * g + 3])};
+        }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+      for (int r0 = 0; r0 < 32; r0 += 8) {
+        const int r = r0 + (lane >> 3), c = lane & 7;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(xp + r * 128 + (c ^ (r & 7)) * 16);
+        const int64_t a = aw + 8 * c;
+        const uint32_t o = a < p.na ? static_cast<uint32_t>(2 * ((32 * j + r) * p.na + a)) : 0x80000000u;
+        __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, o, 0, OUT == kOutStream ? 2 : 0);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+  }
+}
+
+template <int KT, int OUT>
+hipError_t launch_stream(const Prod& p, hipStream_t stream) {
+  const int64_t panels = (p.na + kStreamPanel - 1) / kStreamPanel;
+  const int64_t tiles = (p.nb + kStreamTile - 1) / kStreamTile;
+  const int64_t ranges = panels < 256 ? 256 / panels : 1;  // one workgroup to a CU
+  const int64_t per = (tiles + ranges - 1) / ranges;
+  const int64_t n = panels * ((tiles + per - 1) / per);
+  if (n > 0x7fffffff || per > 0x7fffffff) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((prod_stream_kernel<KT, OUT>), dim3(static_cast<unsigned>(n)), dim3(512), 0, stream, p,
+                     static_cast<int>(per));
+  return hipGetLastError();
+}
+
 template <bool TRB, int OUT>
 hipError_t launch_prod_out(Prod p, hipStream_t stream) {
   const ProdKind kind = prod_kind(TRB, p.na, p.nb, p.K);
@@ -773,6 +975,8 @@ hipError_t launch_prod_out(Prod p, hipStream_t stream) {
     return hipGetLastError();
   }
   if constexpr (TRB) {
+    if (kind == kProdStream)
+      return p.K <= 128 ? launch_stream<2, OUT>(p, stream) : launch_stream<4, OUT>(p, stream);
     return launch_ring<RingShort, TRB, OUT>(p, stream);
   } else {
     if (kind == kProdFew)

@@ -151,6 +151,8 @@ HEAD_CASES = [
     ("bf16", 3, 100, 1, 192, 600, "some"),      # 300 rows: the products' 256 x 256 tiles, short sums
     ("bf16", 11, 50, 1, 264, 3000, "some"),     # both products on 256 x 256 tiles, partial last stages
     ("bf16", 5, 100, 1, 72, 2500, "none"),      # a narrow hidden size: 128-column tiles
+    ("bf16", 3, 67, 1, 1672, 40189, "some"),    # 2^26 weights: dw's stream kernel
+    ("bf16", 1, 40, 2, 1672, 40189, "all"),
     ("fp32", 1, 31, 1, 63, 95, "none"), ("fp32", 1, 33, 1, 65, 97, "none"),
     ("fp32", 2, 64, 3, 250, 3001, "some"),      # sums in several parts
 ]
@@ -280,6 +282,10 @@ EXPAND_CASES = [
     (1, 1, 1, 32), (1, 1, 3, 64), (1, 15, 4, 96), (2, 7, 5, 160), (3, 50, 2, 128), (5, 13, 8, 256),
     (1, 63, 2, 64), (1, 64, 2, 64), (1, 65, 2, 64), (4, 16, 64, 32), (17, 16, 3, 288), (2, 200, 2, 512),
     (5, 129, 2, 320), (9, 100, 4, 544), (1, 128, 5, 256),
+    (1, 1, 1, 288), (1, 16, 3, 288), (1, 17, 2, 512), (1, 64, 1, 544), (1, 129, 2, 288), (1, 255, 2, 320),
+    # 2^26 weights: the weight gradient's stream kernel with 65, 128, 201 and 256 rows, whole and partial
+    # panels of 512 columns
+    (1, 65, 9, 2752), (1, 128, 16, 2080), (3, 67, 8, 2912), (1, 256, 4, 4096),
 ]
 
 
@@ -315,6 +321,26 @@ def test_expander_backward(case):
                             dict(want_dh=False, want_dW=False))):
         alone = D.dbl_expand_branches_backward(h.cuda(), W.cuda(), dout.cuda(), **kw)
         assert torch.equal(alone[i], got[i]) and all(alone[j] is None for j in range(3) if j != i)
+
+
+@pytest.mark.parametrize("case", [(1, 15, 4, 96), (5, 13, 8, 288), (3, 50, 2, 512), (3, 100, 2, 320),
+                                  (9, 100, 4, 544), (3, 67, 8, 2912)], ids=str)
+def test_expander_backward_infinities_stay_infinities(case):
+    """An infinity in the last row, next to what the kernels pad the sums with: the results are infinite
+    where the formula's are, and finite elsewhere."""
+    from paper_2608_05448_amd import dblast as D
+    B, K, R, d = case
+    h, W, dout = _expand_inputs(*case)
+    dout[-1, -1, -1, 5] = float("inf")
+    dout[0, 0, 0, 0] = -float("inf")
+    h, W = torch.where(h == 0, 1.0, h), torch.where(W == 0, 1.0, W)
+    got = D.dbl_expand_branches_backward(h.cuda(), W.cuda(), dout.cuda())
+    do, hd, Wd = (t.cuda().double() for t in (dout.reshape(B * K, R * d), h.reshape(B * K, d), W))
+    dh = do.reshape(B * K, R, d).sum(1) + do @ Wd
+    for t, want in zip(got, (dh.reshape(B, K, d), do.T @ hd, do.sum(0))):
+        inf = torch.isinf(want)
+        assert inf.any() and torch.equal(t.double()[inf], want[inf])
+        assert torch.isfinite(t[torch.isfinite(want)]).all()
 
 
 def test_expander_backward_matches_differences():
