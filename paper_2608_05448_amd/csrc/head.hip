@@ -1794,10 +1794,23 @@ hipError_t launch_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64
 // at d = 4096 300 -> 217, 120 rows 306 -> 242; from 129 rows on two 128-row tiles would stream the
 // weight twice (180 rows at d = 2560 264 us against the ping-pong kernel's 215).
 constexpr int64_t kFewRows = 128;
+// Training batches of any size meet vocabularies of any size: fewer than kFewTiles tiles leave CUs idle, and
+// the next smaller tiles are taken (us, rows x ids, d, by tile: 256 x 256, 256 x 128, 128 x 128 ids x rows:
+// 320 x 6706, 2560: 49, 40, 33; 978 x 3456, 2560: 49, 47, 34; 460 x 14360, 2048: 44, 38, 51; 1079 x 6264,
+// 4096: 78, 69, 94; 600 x 20000, 1024, 237 of the largest: 32, 41, 57).
+using HeadFew128Short = FewCfg<128, 128, 1, 4, 1, 4>;
+inline bool few_tiles(int64_t V, int64_t M, int bv, int bm) {
+  return ((V + bv - 1) / bv) * ((M + bm - 1) / bm) < kFewTiles;
+}
 template <int EPI, bool TAIL>
 hipError_t launch_head_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64_t M, int64_t V,
                            int d, hipStream_t stream) {
-  if (M > HeadFew64::BM) return launch_few<HeadFew128, EPI, TAIL>(h, w, ea, M, V, d, stream);
+  if (M > HeadFew64::BM) {
+    if constexpr (epi_train(EPI))
+      if (few_tiles(V, M, HeadFew128::BV, HeadFew128::BM))
+        return launch_few<HeadFew128Short, EPI, TAIL>(h, w, ea, M, V, d, stream);
+    return launch_few<HeadFew128, EPI, TAIL>(h, w, ea, M, V, d, stream);
+  }
   if ((V + HeadFew64::BV - 1) / HeadFew64::BV >= kFewTiles)
     return launch_few<HeadFew64, EPI, TAIL>(h, w, ea, M, V, d, stream);
   return launch_few<HeadFew64Short, EPI, TAIL>(h, w, ea, M, V, d, stream);
@@ -1811,7 +1824,9 @@ hipError_t launch_head_gemm(const __bf16* h, const __bf16* w, const EpiArgs& ea,
                             int d, hipStream_t stream) {
   if (d % 64 == 0 && M <= kFewRows) return launch_head_few<EPI, false>(h, w, ea, M, V, d, stream);
   if constexpr (epi_train(EPI))
-    if (M <= kFewRows) return launch_head_few<EPI, true>(h, w, ea, M, V, d, stream);
+    if (M <= kFewRows || few_tiles(V, M, PpCfg::BV, PpCfg::BM))
+      return d % 64 == 0 ? launch_head_few<EPI, false>(h, w, ea, M, V, d, stream)
+                         : launch_head_few<EPI, true>(h, w, ea, M, V, d, stream);
   static_assert(PpCfg::BM == 256 && PpCfg::BV == 256 && DCfg::BM == 256 && DCfg::BV == 256 &&
                     Cfg::BM == 256 && Cfg::BV == 256, "one grid for the 256 x 256 tiles");
   const int64_t dm = (M + 255) / 256;

@@ -153,6 +153,9 @@ HEAD_CASES = [
     ("bf16", 5, 100, 1, 72, 2500, "none"),      # a narrow hidden size: 128-column tiles
     ("bf16", 3, 67, 1, 1672, 40189, "some"),    # 2^26 weights: dw's stream kernel
     ("bf16", 1, 40, 2, 1672, 40189, "all"),
+    ("bf16", 6, 50, 1, 128, 45000, "some"),     # 300 rows by tile of the head: 256 x 256, 256 x 128 and
+    ("bf16", 6, 50, 1, 136, 15000, "some"),     # 128 x 128 (the smaller vocabularies above), 100 rows
+    ("bf16", 2, 50, 1, 136, 42000, "some"),
     ("fp32", 1, 31, 1, 63, 95, "none"), ("fp32", 1, 33, 1, 65, 97, "none"),
     ("fp32", 2, 64, 3, 250, 3001, "some"),      # sums in several parts
 ]
