@@ -652,73 +652,78 @@ __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
                         : (64 * wb + 32 * j + (lane & 31)) * 128);
   const int bx = 16 * (half ^ row_swz(lane & 31));
   bf16x8 af[2][NRA], bf[2][NCB];
-  auto load_frags = [&](int aslot, int bslot, int kk0, int left) {
+  auto load_frags = [&](int aslot, int bslot, int kk, int ks) {  // k step kk of a stage, to set ks
     const char* sa = smem + aslot * TILE;
     const char* sb = smem + bslot * TILE;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-#pragma unroll
-      for (int i = 0; i < NRA; ++i) {
-        const char* q = sa + fa[i] + (kk0 + ks) * 8192;
-        af[ks][i] = join(lds_read_tr(q), lds_read_tr(q + 2048));
-      }
-#pragma unroll
-      for (int j = 0; j < NCB; ++j) {
-        if constexpr (TRB) {
-          const char* q = sb + fb[j] + (kk0 + ks) * 8192;
-          bf[ks][j] = join(lds_read_tr(q), lds_read_tr(q + 2048));
-        } else {
-          bf[ks][j] = *reinterpret_cast<const bf16x8*>(sb + fb[j] + ((32 * (kk0 + ks)) ^ bx));
-        }
-      }
+    for (int i = 0; i < NRA; ++i) {
+      const char* q = sa + fa[i] + kk * 8192;
+      af[ks][i] = join(lds_read_tr(q), lds_read_tr(q + 2048));
     }
-    if (left < 64) {  // both operands: what a copy past the end repeats may hold infinities
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        const int n = left - 16 * (kk0 + ks) - 8 * half;
-#pragma unroll
-        for (int i = 0; i < NRA; ++i) af[ks][i] = keep_first(af[ks][i], n);
-#pragma unroll
-        for (int j = 0; j < NCB; ++j) bf[ks][j] = keep_first(bf[ks][j], n);
+    for (int j = 0; j < NCB; ++j) {
+      if constexpr (TRB) {
+        const char* q = sb + fb[j] + kk * 8192;
+        bf[ks][j] = join(lds_read_tr(q), lds_read_tr(q + 2048));
+      } else {
+        bf[ks][j] = *reinterpret_cast<const bf16x8*>(sb + fb[j] + ((32 * kk) ^ bx));
       }
     }
   };
-  auto compute = [&]() {
+  // Both operands: what a copy past the end repeats may hold infinities.
+  auto mask = [&](int kk0, int left) {
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
+    for (int ks = 0; ks < 2; ++ks) {
+      const int n = left - 16 * (kk0 + ks) - 8 * half;
 #pragma unroll
-      for (int i = 0; i < NRA; ++i)
+      for (int i = 0; i < NRA; ++i) af[ks][i] = keep_first(af[ks][i], n);
 #pragma unroll
-        for (int j = 0; j < NCB; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks][i], bf[ks][j], acc[i][j], 0, 0, 0);
+      for (int j = 0; j < NCB; ++j) bf[ks][j] = keep_first(bf[ks][j], n);
+    }
+  };
+  auto mfmas = [&](int ks) {
+#pragma unroll
+    for (int i = 0; i < NRA; ++i)
+#pragma unroll
+      for (int j = 0; j < NCB; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[ks][i], bf[ks][j], acc[i][j], 0, 0, 0);
   };
 
-  const int H = 2 * nk;  // turns per group
-  // Turn t: its memory half (fragments of k half t % 2 of stage s = t / 2, and the turn's copies into
-  // slots that stage s - 1 has left), a barrier, its compute half, a barrier. Group 1 runs one barrier
-  // behind group 0, so that each half of one group meets the other half of the other. At odd turns every
-  // wave waits for its own copies of stage s + 1 (all but the 4 of stage s + 2 just issued) before the
-  // barrier that opens the first memory half that reads stage s + 1.
-  auto turn = [&](int t, int a3, int b2) {  // a3 = (t / 2) % 3, b2 = (t / 2) % 2
-    const int s = t >> 1;
-    load_frags(a3, b2, (t & 1) * 2, s == nk - 1 ? last : 64);
-    if (!(t & 1)) {
-      if (t >= 2 && s + 1 < nk) copy_B(s + 1, b2 ^ 1);
+  // Turns 2 s and 2 s + 1 take a stage's halves. A turn: its memory half (fragments, and copies into slots
+  // that stage s - 1 has left), a barrier, its compute half, a barrier. Group 1 runs one barrier behind
+  // group 0, so that each half of one group meets the other half of the other. The first fragments of an
+  // odd turn are read in the even turn's compute half, into registers that its first MFMAs have left: with
+  // all 24 transposing reads in one memory half that half was the longer one. At odd turns every wave
+  // waits for its own copies of stage s + 1 (all but the 4 of stage s + 2 just issued) before the barrier
+  // that opens the first memory half that reads stage s + 1.
+  auto turn = [&](auto odd_c, int s, int a3, int b2) {  // a3 = s % 3, b2 = s % 2
+    constexpr bool odd = decltype(odd_c)::value;
+    if constexpr (!odd) load_frags(a3, b2, 0, 0);
+    load_frags(a3, b2, odd ? 3 : 1, 1);
+    if constexpr (!odd) {
+      if (s >= 1 && s + 1 < nk) copy_B(s + 1, b2 ^ 1);
     } else {
       if (s + 2 < nk) copy_A(s + 2, a3 == 0 ? 2 : a3 - 1);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if ((t & 1) && grp == 1) {
+    if (s == nk - 1 && last < 64) mask(odd ? 2 : 0, last);
+    if (odd && grp == 1) {
       if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
     }
     pp_barrier();
     __builtin_amdgcn_s_setprio(1);  // the computing wave issues before its neighbour's copies and reads
-    compute();
+    mfmas(0);
+    if constexpr (!odd) {
+      __builtin_amdgcn_sched_barrier(0);
+      load_frags(a3, b2, 2, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    mfmas(1);
     __builtin_amdgcn_s_setprio(0);
-    if ((t & 1) && grp == 0) {
+    if (odd && grp == 0) {
       if (s + 2 < nk) wait_vmcnt<4>(); else wait_vmcnt<0>();
     }
-    if (!(grp == 1 && t == H - 1)) pp_barrier();
+    if (!(grp == 1 && odd && s == nk - 1)) pp_barrier();
   };
   if (nk > 0) {
     copy_A(0, 0);
@@ -733,9 +738,9 @@ __global__ __launch_bounds__(512, 1) void prod_pp_kernel(const Prod p) {
     pp_barrier();
     if (grp == 1) pp_barrier();
     int a3 = 0;
-    for (int t = 0; t < H; t += 2) {
-      turn(t, a3, (t >> 1) & 1);
-      turn(t + 1, a3, (t >> 1) & 1);
+    for (int s = 0; s < nk; ++s) {
+      turn(std::false_type{}, s, a3, s & 1);
+      turn(std::true_type{}, s, a3, s & 1);
       a3 = a3 == 2 ? 0 : a3 + 1;
     }
   }
