@@ -71,7 +71,7 @@ __device__ __forceinline__ int tensor_of(const Set& s, int count, int c) {
 }
 
 // STREAM: non-temporal loads. A set that the 256 MB Infinity Cache cannot hold until it is clipped is read
-// faster so (2.6 GB 514 -> 453 us); one that it can hold is then clipped from it (52 MB 18.2 us, 20.8 with
+// faster so (3.0 GB 514 -> 453 us); one that it can hold is then clipped from it (52 MB 18.2 us, 20.8 with
 // the norm's loads non-temporal). More workgroups or loads in flight, smaller and larger chunks and
 // non-temporal accesses in the clipping gained nothing.
 constexpr int64_t kStreamBytes = int64_t(512) << 20;
