@@ -413,8 +413,9 @@ dbl_status dbl_early_determinism(int64_t M, int64_t b, int64_t V, const int32_t*
  *   x     [B, K] int32 tokens
  *   nll   out [B, K, R] fp32;  lse  out [B, K, R] fp32
  *   ws    workspace of dbl_workspace_bytes(DBL_OP_HEAD_NLL, shape) bytes
- * Errors: DBL_EINVAL for null or misaligned pointers, DBL_EDTYPE, DBL_ESHAPE (also for
- * B*K*R >= 2^31), DBL_EWORKSPACE.
+ * nll and lse may overlap neither each other nor an input. Errors: DBL_EINVAL for null, misaligned or
+ * overlapping pointers, DBL_EDTYPE, DBL_ESHAPE (also for B*K*R >= 2^24), DBL_EWORKSPACE, DBL_EHIP (also
+ * where a launch would need 2^32 threads: B*K*R*V from about 2^37 on).
  */
 dbl_status dbl_head_nll(dbl_shape shape, int dt, const void* h, const void* w, const int32_t* x,
                         float* nll, float* lse, void* ws, size_t ws_bytes, void* stream);
@@ -444,7 +445,7 @@ dbl_status dbl_head_nll_backward(dbl_shape shape, int dt, const void* h, const v
  *     dh[b, k]   = sum_z (dout[b, k, z] + W_z^T dout[b, k, z]),
  *     dW[z*d + i, j] = sum_{b,k} dout[b, k, z, i] h[b, k, j],   dc[z*d + i] = sum_{b,k} dout[b, k, z, i]
  * with fp32 accumulation, each rounded once to bf16.
- *   shape   B, K, R, d used (V unused); d % 32 == 0, R*d <= 2^23
+ *   shape   B, K, R, d used (V unused); d % 32 == 0, R*d <= 2^23, B*K < 2^24
  *   h       [B, K, d] bf16 trunk states;  W  [R*d, d] bf16;  dout  [B, K, R, d] bf16
  *   dh      out [B, K, d] bf16 or NULL;  dW  out [R*d, d] bf16 or NULL;  dc  out [R*d] bf16 or NULL
  *   ws      workspace of dbl_workspace_bytes(DBL_OP_EXPAND_BACKWARD, shape) bytes (V = 1), needed for dh;
@@ -466,7 +467,7 @@ dbl_status dbl_expand_branches_backward(dbl_shape shape, const void* h, const vo
  *           anywhere); a tensor of 0 elements may be NULL
  *   numel   [n] numbers of elements >= 0, less than 2^40 together
  *   dt      [n] DBL_F32 or DBL_BF16
- *   norm    out: one fp32 (device)
+ *   norm    out: one fp32 (device), in none of the tensors
  *   ws      workspace of dbl_workspace_bytes(DBL_OP_GRAD_NORM, shape) bytes, shape.B = n and 1 elsewhere
  * Errors: DBL_EINVAL, DBL_ESHAPE, DBL_EDTYPE, DBL_EWORKSPACE.
  */

@@ -43,7 +43,7 @@ dbl_status check_nll(const dbl_shape& s, int dt) {
   if (dt != DBL_BF16 && dt != DBL_F32) return fail(DBL_EDTYPE, "dt must be DBL_BF16 or DBL_F32");
   if (dt == DBL_BF16 && s.d % 8 != 0) return fail(DBL_ESHAPE, "bf16 head needs d % 8 == 0");
   if (static_cast<double>(s.B) * s.K * s.R > static_cast<double>(dbl::kMaxTrainRows))
-    return fail(DBL_ESHAPE, "B*K*R must be < 2^31");
+    return fail(DBL_ESHAPE, "B*K*R must be < 2^24");
   return ok();
 }
 
@@ -115,6 +115,12 @@ dbl_status dbl_head_nll(dbl_shape s, int dt, const void* h, const void* w, const
     if (!w || (s.B > 0 && (!h || !x || !nll || !lse))) return fail(DBL_EINVAL, "NULL pointer");
     if (dbl_status st = check_aligned({{h, "h"}, {w, "w"}, {x, "x"}, {nll, "nll"}, {lse, "lse"}}))
       return st;
+    const size_t e = dt == DBL_BF16 ? 2 : 4;
+    const size_t rows = static_cast<size_t>(s.B) * s.K * s.R;
+    std::vector<Span> spans = {{h, rows * s.d * e, false}, {w, static_cast<size_t>(s.V) * s.d * e, false},
+                               {x, size_t(4) * s.B * s.K, false}, {nll, 4 * rows, true},
+                               {lse, 4 * rows, true}};
+    if (overlapping(spans)) return fail(DBL_EINVAL, "nll and lse must not overlap another array");
     if (s.B == 0) return ok();
     WsLayout L;
     if (dbl_status st = check_ws(DBL_OP_HEAD_NLL, s, ws, ws_bytes, &L)) return st;
@@ -176,7 +182,7 @@ dbl_status dbl_expand_branches_backward(dbl_shape s, const void* h, const void* 
     if (s.d < 32 || s.d % 32 != 0 || s.d > (int64_t(1) << 20) || s.R * s.d > (int64_t(1) << 23))
       return fail(DBL_ESHAPE, "expander needs d % 32 == 0, 32 <= d <= 2^20 and R*d <= 2^23");
     if (static_cast<double>(s.B) * s.K > static_cast<double>(dbl::kMaxTrainRows))
-      return fail(DBL_ESHAPE, "B*K must be < 2^31");
+      return fail(DBL_ESHAPE, "B*K must be < 2^24");
     if (!W || (s.B > 0 && (!h || !dout))) return fail(DBL_EINVAL, "NULL input pointer");
     if (s.B > 0 && !dh && !dW && !dc) return fail(DBL_EINVAL, "no output");
     if (dbl_status st = check_aligned({{h, "h"}, {W, "W"}, {dout, "dout"}, {dh, "dh"}, {dW, "dW"},
@@ -217,6 +223,12 @@ dbl_status dbl_grad_norm(int64_t n, const void* const* grads, const int64_t* num
     if (dbl_status st = check_tensors(n, grads, numel, dt, nullptr, false, &t)) return st;
     if (!norm || reinterpret_cast<uintptr_t>(norm) % 4 != 0)
       return fail(DBL_EINVAL, "norm is NULL or misaligned");
+    const uintptr_t to = reinterpret_cast<uintptr_t>(norm);
+    for (const dbl::GradTensor& g : t) {
+      const uintptr_t at = reinterpret_cast<uintptr_t>(g.g);
+      if (g.n > 0 && to + 4 > at && to < at + static_cast<uintptr_t>(g.n) * (g.bf16 ? 2 : 4))
+        return fail(DBL_EINVAL, "norm overlaps a tensor");
+    }
     WsLayout L;
     if (dbl_status st = check_ws(DBL_OP_GRAD_NORM, dbl_shape{n, 1, 1, 1, 1}, ws, ws_bytes, &L))
       return st;

@@ -374,7 +374,7 @@ __device__ __forceinline__ void tile_nll_store(f32x16 (&acc)[NRB][NCB], const Ep
 #pragma unroll
     for (int i = 0; i < NRB * 16; ++i) mx = fmaxf(mx, x[i]);
     mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float nb = -mx * kLog2e;
+    const float nb = mx > -INFINITY ? -mx * kLog2e : 0.0f;  // a tile of logits of minus infinity: mass 0
     float s = 0.0f;
 #pragma unroll
     for (int i = 0; i < NRB * 16; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, nb));
@@ -1238,7 +1238,7 @@ __device__ __forceinline__ void pp_barrier() {
 }
 
 // TAIL: d % 8 == 0 only. The last stage holds `last` < 64 units: chunks past them fetch the row's first
-// chunk of the stage, and meet zeros in the branch rows' fragments.
+// chunk of the stage, and count as 0 in both operands' fragments (what they repeat may be infinite).
 template <int EPI, bool TAIL = false>
 __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
     const __bf16* __restrict__ h, const __bf16* __restrict__ w, const EpiArgs ea, int64_t M,
@@ -1337,10 +1337,13 @@ __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
     if constexpr (TAIL)
       if (left < C::BK) {
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks)
+        for (int ks = 0; ks < 2; ++ks) {
+          const int n = left - 16 * (kk0 + ks);
 #pragma unroll
-          for (int cb = 0; cb < NCB; ++cb)
-            bfr[ks][cb] = first_units(bfr[ks][cb], left - 16 * (kk0 + ks), lane);
+          for (int rb = 0; rb < NRB; ++rb) af[ks][rb] = first_units(af[ks][rb], n, lane);
+#pragma unroll
+          for (int cb = 0; cb < NCB; ++cb) bfr[ks][cb] = first_units(bfr[ks][cb], n, lane);
+        }
       }
   };
   auto compute = [&]() {
@@ -1555,6 +1558,8 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
         bfr[cb] = *reinterpret_cast<const bf16x8*>(blk + b_base + cb * 32 * ROWB + x);
       if constexpr (TAIL)
         if (kt == nk - 1) {
+#pragma unroll
+          for (int rb = 0; rb < NRB; ++rb) af[rb] = first_units(af[rb], last - 16 * ks, lane);
 #pragma unroll
           for (int cb = 0; cb < NCB; ++cb) bfr[cb] = first_units(bfr[cb], last - 16 * ks, lane);
         }
@@ -1783,7 +1788,7 @@ hipError_t launch_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, int64
                       int d, hipStream_t stream) {
   const int64_t dm = (M + C::BM - 1) / C::BM;
   const int64_t nwg = ((V + C::BV - 1) / C::BV) * dm;
-  if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (nwg > kMaxThreads / C::kThreads) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((head_bf16_few_kernel<C, EPI, TAIL>), dim3(static_cast<unsigned>(nwg)),
                      dim3(C::kThreads), 0, stream, h, w, ea, M, V, d, static_cast<int>(dm));
   return hipGetLastError();
@@ -1831,7 +1836,7 @@ hipError_t launch_head_gemm(const __bf16* h, const __bf16* w, const EpiArgs& ea,
                     Cfg::BM == 256 && Cfg::BV == 256, "one grid for the 256 x 256 tiles");
   const int64_t dm = (M + 255) / 256;
   const int64_t nwg = ((V + 255) / 256) * dm;
-  if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (nwg > kMaxThreads / PpCfg::kThreads) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<unsigned>(nwg));
   const int n_mtiles = static_cast<int>(dm);
   if (d % PpCfg::BK == 0) {

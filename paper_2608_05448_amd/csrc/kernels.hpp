@@ -283,7 +283,8 @@ inline int grad_splits_f32(int64_t na, int64_t nb, int64_t K) {
   return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
 }
 
-constexpr int64_t kMaxTrainRows = 0x7fffffff;
+constexpr int64_t kMaxThreads = 0xffffffffll;     // of a launch
+constexpr int64_t kMaxTrainRows = (1 << 24) - 1;  // a workgroup of 256 each
 
 constexpr int kNormSet = 180;      // tensors of one launch of the gradient norm
 constexpr int kNormBlocks = 1024;  // its workgroups, and partial sums, at most

@@ -768,7 +768,7 @@ template <class C, bool TRB, int OUT>
 hipError_t launch_ring(Prod p, hipStream_t stream) {
   const int64_t na = (p.na + C::BA - 1) / C::BA, nb = (p.nb + C::BB - 1) / C::BB;
   const int64_t n = na * nb * p.splits;
-  if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (n > kMaxThreads / C::kThreads) return hipErrorInvalidConfiguration;
   p.n_btiles = static_cast<int>(nb);
   hipLaunchKernelGGL((prod_ring_kernel<C, TRB, OUT>), dim3(static_cast<unsigned>(n)),
                      dim3(C::kThreads), 0, stream, p);
@@ -962,7 +962,7 @@ hipError_t launch_stream(const Prod& p, hipStream_t stream) {
   const int64_t ranges = panels < 256 ? 256 / panels : 1;  // one workgroup to a CU
   const int64_t per = (tiles + ranges - 1) / ranges;
   const int64_t n = panels * ((tiles + per - 1) / per);
-  if (n > 0x7fffffff || per > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (n > kMaxThreads / 512 || per > 0x7fffffff) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((prod_stream_kernel<KT, OUT>), dim3(static_cast<unsigned>(n)), dim3(512), 0, stream, p,
                      static_cast<int>(per));
   return hipGetLastError();
@@ -973,7 +973,7 @@ hipError_t launch_prod_out(Prod p, hipStream_t stream) {
   const ProdKind kind = prod_kind(TRB, p.na, p.nb, p.K);
   if (kind == kProdPp) {
     const int64_t na = (p.na + 255) / 256, nb = (p.nb + 255) / 256, n = na * nb * p.splits;
-    if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (n > kMaxThreads / 512) return hipErrorInvalidConfiguration;
     p.n_btiles = static_cast<int>(nb);
     hipLaunchKernelGGL((prod_pp_kernel<TRB, OUT>), dim3(static_cast<unsigned>(n)), dim3(512), 0, stream,
                        p);
@@ -1208,9 +1208,10 @@ __global__ __launch_bounds__(256) void gemm_f32_kernel(const F32Args p) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) mx = fmaxf(mx, x[r]);
         mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float top = mx > -INFINITY ? mx : 0.0f;  // logits of minus infinity only: mass 0
         float s = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s += __expf(x[r] - mx);
+        for (int r = 0; r < 16; ++r) s += __expf(x[r] - top);
         s += __shfl_xor(s, 32);
         if (b < nb && half == 0) p.lmass[b * p.nT + aw / 32 + i] = mx + logf(s);
       }
@@ -1240,7 +1241,7 @@ template <bool TRA, bool TRB, int EPI, int ROWS>
 hipError_t launch_f32_rows(F32Args p, hipStream_t stream) {
   const int64_t na = (p.na + 127) / 128, nb = (p.nb + ROWS - 1) / ROWS;
   const int64_t n = na * nb * p.splits;
-  if (n > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (n > kMaxThreads / 256) return hipErrorInvalidConfiguration;
   p.n_btiles = static_cast<int>(nb);
   hipLaunchKernelGGL((gemm_f32_kernel<TRA, TRB, EPI, ROWS>), dim3(static_cast<unsigned>(n)), dim3(256), 0,
                      stream, p);
@@ -1303,26 +1304,27 @@ __global__ __launch_bounds__(64) void dh_finish_kernel(const NllArgs a, int64_t 
 }
 
 // The expander's trunk gradient (the product's parts and the residual path's R branch gradients, in fp32,
-// rounded once) and bias gradient, in one launch: the first n_dh workgroups take four blocks of 256 columns
-// of trunk rows, the others 64 features each.
+// rounded once) and bias gradient, in one launch: the first n_dh workgroups take blocks of 256 columns of
+// trunk rows, one a wave at a time, the others 64 features each.
 __global__ __launch_bounds__(256) void expand_finish_kernel(const ExpandBackwardArgs a, int64_t n_dh) {
   const int d = a.d, R = static_cast<int>(a.R);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (blockIdx.x < n_dh) {
     const int blocks = (d + 255) / 256;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    const int64_t p = at / blocks;
-    const int j = static_cast<int>(at % blocks) * 256 + 4 * lane;
-    if (p >= a.P || j >= d) return;
-    const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d + j;
-    f32x4 v = sum_parts(a.part + p * d + j, a.P * d, a.splits);
+    for (int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + wave; at < a.P * blocks; at += n_dh * 4) {
+      const int64_t p = at / blocks;
+      const int j = static_cast<int>(at % blocks) * 256 + 4 * lane;
+      if (j >= d) continue;
+      const __bf16* g = static_cast<const __bf16*>(a.dout) + p * R * d + j;
+      f32x4 v = sum_parts(a.part + p * d + j, a.P * d, a.splits);
 #pragma unroll 8
-    for (int z = 0; z < R; ++z) {
-      const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d);
+      for (int z = 0; z < R; ++z) {
+        const bf16x4 u = *reinterpret_cast<const bf16x4*>(g + static_cast<int64_t>(z) * d);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
+        for (int q = 0; q < 4; ++q) v[q] += static_cast<float>(u[q]);
+      }
+      store4(static_cast<__bf16*>(a.dh) + p * d + j, v);
     }
-    store4(static_cast<__bf16*>(a.dh) + p * d + j, v);
     return;
   }
   // dc: the sum over the trunk rows of every branch feature's gradient, 32 rows side by side.
@@ -1354,6 +1356,101 @@ __global__ __launch_bounds__(256) void expand_finish_kernel(const ExpandBackward
     static_cast<__bf16*>(a.dc)[j0 + threadIdx.x] =
         static_cast<__bf16>((part[0][threadIdx.x] + part[1][threadIdx.x]) +
                             (part[2][threadIdx.x] + part[3][threadIdx.x]));
+}
+
+// Ids v0 .. v0 + n - 1 of the backward pass: their part of the logits' gradient, added to the sums of dh, and
+// their rows of dw. Without rows (M = 0) only dw is written: products over no terms.
+hipError_t nll_piece_bf16(const NllArgs& a, int64_t v0, int64_t n, hipStream_t stream) {
+  const int64_t M = a.P * a.R;
+  const __bf16* w = static_cast<const __bf16*>(a.w) + v0 * a.d;
+  if (M > 0) {
+    HeadTrainArgs h{};
+    h.M = M;
+    h.V = n;
+    h.d = a.d;
+    h.h = a.hc;
+    h.w = w;
+    h.count = a.count;
+    h.rows = a.rows;
+    h.grad = a.grad;
+    h.ldg = a.piece;
+    h.vbase = v0;
+    hipError_t e = launch_head_train(h, true, stream);
+    if (e != hipSuccess) return e;
+    Prod p{};
+    p.A = w;
+    p.lda = p.na = a.d;
+    p.B = static_cast<const __bf16*>(a.grad);
+    p.ldb = a.piece;
+    p.nb = M;
+    p.K = n;
+    p.count = a.count;
+    p.part = a.part;
+    p.part_stride = M * a.d;
+    p.accumulate = v0 > 0;
+    p.splits = a.splits;
+    e = launch_prod_part(p, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (!a.dw) return hipSuccess;
+  Prod q{};
+  q.A = static_cast<const __bf16*>(a.hs);
+  q.lda = q.na = a.d;
+  q.B = static_cast<const __bf16*>(a.grad);
+  q.ldb = a.piece;
+  q.nb = n;
+  q.K = M;
+  q.count = M > 0 ? a.count : nullptr;
+  q.out = static_cast<__bf16*>(a.dw) + v0 * a.d;
+  q.splits = 1;
+  return launch_prod(q, stream);
+}
+
+hipError_t nll_piece_f32(const NllArgs& a, int64_t v0, int64_t n, hipStream_t stream) {
+  const int64_t M = a.P * a.R;
+  const float* w = static_cast<const float*>(a.w) + v0 * a.d;
+  if (M > 0) {
+    F32Args p{};
+    p.A = w;
+    p.B = static_cast<const float*>(a.hc);
+    p.lda = p.ldb = p.K = a.d;
+    p.na = n;
+    p.nb = M;
+    p.count_b = a.count;
+    p.splits = 1;
+    p.rows = a.rows;
+    p.grad = static_cast<float*>(a.grad);
+    p.ldg = a.piece;
+    p.vbase = v0;
+    hipError_t e = launch_f32<false, false, kF32Grad>(p, stream);
+    if (e != hipSuccess) return e;
+    F32Args q{};
+    q.A = w;
+    q.lda = q.na = a.d;
+    q.B = static_cast<const float*>(a.grad);
+    q.ldb = a.piece;
+    q.nb = M;
+    q.K = n;
+    q.count_b = a.count;
+    q.part = a.part;
+    q.part_stride = M * a.d;
+    q.accumulate = v0 > 0;
+    q.splits = a.splits;
+    e = launch_f32<true, false, kF32Part>(q, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (!a.dw) return hipSuccess;
+  F32Args r{};
+  r.A = static_cast<const float*>(a.hs);
+  r.lda = r.na = a.d;
+  r.B = static_cast<const float*>(a.grad);
+  r.ldb = a.piece;
+  r.nb = n;
+  r.K = M;
+  r.count_k = M > 0 ? a.count : nullptr;
+  r.out = static_cast<float*>(a.dw) + v0 * a.d;
+  r.splits = 1;
+  return launch_f32<true, true, kF32Out>(r, stream);
 }
 
 }  // namespace
@@ -1398,110 +1495,21 @@ hipError_t launch_nll(const NllArgs& a, hipStream_t stream) {
 
 hipError_t launch_nll_backward(const NllArgs& a, hipStream_t stream) {
   const int64_t M = a.P * a.R;
-  hipError_t e = hipSuccess;
-  if (M > 0) e = gather_rows(a, stream);  // without rows dw is 0: a product over no terms
-  if (e != hipSuccess) return e;
-  const int64_t part_stride = M * a.d;
+  if (M > 0) {
+    const hipError_t e = gather_rows(a, stream);
+    if (e != hipSuccess) return e;
+  }
   for (int64_t v0 = 0; v0 < a.V; v0 += a.piece) {
     const int64_t n = a.V - v0 < a.piece ? a.V - v0 : a.piece;
-    if (a.bf16) {
-      const __bf16* w = static_cast<const __bf16*>(a.w) + v0 * a.d;
-      if (M > 0) {
-      HeadTrainArgs h{};
-      h.M = M;
-      h.V = n;
-      h.d = a.d;
-      h.h = a.hc;
-      h.w = w;
-      h.count = a.count;
-      h.rows = a.rows;
-      h.grad = a.grad;
-      h.ldg = a.piece;
-      h.vbase = v0;
-      e = launch_head_train(h, true, stream);
-      if (e != hipSuccess) return e;
-      Prod p{};
-      p.A = w;
-      p.lda = p.na = a.d;
-      p.B = static_cast<const __bf16*>(a.grad);
-      p.ldb = a.piece;
-      p.nb = M;
-      p.K = n;
-      p.count = a.count;
-      p.part = a.part;
-      p.part_stride = part_stride;
-      p.accumulate = v0 > 0;
-      p.splits = a.splits;
-      e = launch_prod_part(p, stream);
-      if (e != hipSuccess) return e;
-      }
-      if (a.dw) {
-        Prod q{};
-        q.A = static_cast<const __bf16*>(a.hs);
-        q.lda = q.na = a.d;
-        q.B = static_cast<const __bf16*>(a.grad);
-        q.ldb = a.piece;
-        q.nb = n;
-        q.K = M;
-        q.count = M > 0 ? a.count : nullptr;
-        q.out = static_cast<__bf16*>(a.dw) + v0 * a.d;
-        q.splits = 1;
-        e = launch_prod(q, stream);
-      }
-    } else {
-      const float* w = static_cast<const float*>(a.w) + v0 * a.d;
-      if (M > 0) {
-      F32Args p{};
-      p.A = w;
-      p.B = static_cast<const float*>(a.hc);
-      p.lda = p.ldb = p.K = a.d;
-      p.na = n;
-      p.nb = M;
-      p.count_b = a.count;
-      p.splits = 1;
-      p.rows = a.rows;
-      p.grad = static_cast<float*>(a.grad);
-      p.ldg = a.piece;
-      p.vbase = v0;
-      e = launch_f32<false, false, kF32Grad>(p, stream);
-      if (e != hipSuccess) return e;
-      F32Args q{};
-      q.A = w;
-      q.lda = q.na = a.d;
-      q.B = static_cast<const float*>(a.grad);
-      q.ldb = a.piece;
-      q.nb = M;
-      q.K = n;
-      q.count_b = a.count;
-      q.part = a.part;
-      q.part_stride = part_stride;
-      q.accumulate = v0 > 0;
-      q.splits = a.splits;
-      e = launch_f32<true, false, kF32Part>(q, stream);
-      if (e != hipSuccess) return e;
-      }
-      if (a.dw) {
-        F32Args r{};
-        r.A = static_cast<const float*>(a.hs);
-        r.lda = r.na = a.d;
-        r.B = static_cast<const float*>(a.grad);
-        r.ldb = a.piece;
-        r.nb = n;
-        r.K = M;
-        r.count_k = M > 0 ? a.count : nullptr;
-        r.out = static_cast<float*>(a.dw) + v0 * a.d;
-        r.splits = 1;
-        e = launch_f32<true, true, kF32Out>(r, stream);
-      }
-    }
+    const hipError_t e = a.bf16 ? nll_piece_bf16(a, v0, n, stream) : nll_piece_f32(a, v0, n, stream);
     if (e != hipSuccess) return e;
   }
   if (M == 0) return hipSuccess;
   const dim3 grid(static_cast<unsigned>(M), static_cast<unsigned>((a.d + 255) / 256));
   if (a.bf16)
-    hipLaunchKernelGGL(dh_finish_kernel<__bf16>, grid, dim3(64), 0, stream, a, part_stride);
+    hipLaunchKernelGGL(dh_finish_kernel<__bf16>, grid, dim3(64), 0, stream, a, M * a.d);
   else
-    hipLaunchKernelGGL(dh_finish_kernel<float>, grid, dim3(64), 0, stream, a, part_stride);
+    hipLaunchKernelGGL(dh_finish_kernel<float>, grid, dim3(64), 0, stream, a, M * a.d);
   return hipGetLastError();
 }
 
@@ -1535,10 +1543,10 @@ hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t strea
     e = launch_prod(q, stream);
     if (e != hipSuccess) return e;
   }
-  const int64_t n_dh = a.dh ? (a.P * ((a.d + 255) / 256) + 3) / 4 : 0;
-  const int64_t blocks = n_dh + (a.dc ? (n + 63) / 64 : 0);
+  int64_t n_dh = a.dh ? (a.P * ((a.d + 255) / 256) + 3) / 4 : 0;
+  n_dh = n_dh < 1 << 20 ? n_dh : 1 << 20;
+  const int64_t blocks = n_dh + (a.dc ? (n + 63) / 64 : 0);  // at most 2^20 + 2^17
   if (blocks == 0) return hipSuccess;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(expand_finish_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, a,
                      n_dh);
   return hipGetLastError();

@@ -144,11 +144,15 @@ int main(int argc, char** argv) {
                          nullptr) == DBL_EINVAL);
     }
   }
+  CHECK(dbl_head_nll(hs, DBL_BF16, P(a(0)), P(a(1)), I(a(2)), F(a(3)), F(a(3)), P(a(20)), fws, nullptr) ==
+        DBL_EINVAL);
+  CHECK(dbl_head_nll(hs, DBL_BF16, P(a(0)), P(a(1)), I(a(2)), F(a(3)), F(a(1) + 16), P(a(20)), fws,
+                     nullptr) == DBL_EINVAL);
   CHECK(dbl_head_nll(dbl_shape{2, 4, 3, 60, 1000}, DBL_BF16, P(a(0)), P(a(1)), I(a(2)), F(a(3)),
                      F(a(4)), P(a(20)), fws, nullptr) == DBL_ESHAPE);
   CHECK(dbl_head_nll(hs, 5, P(a(0)), P(a(1)), I(a(2)), F(a(3)), F(a(4)), P(a(20)), fws, nullptr) ==
         DBL_EDTYPE);
-  CHECK(dbl_head_nll(dbl_shape{1 << 22, 1 << 10, 1, 8, 8}, DBL_BF16, P(a(0)), P(a(1)), I(a(2)),
+  CHECK(dbl_head_nll(dbl_shape{1 << 14, 1 << 10, 1, 8, 8}, DBL_BF16, P(a(0)), P(a(1)), I(a(2)),
                      F(a(3)), F(a(4)), P(a(20)), bad, nullptr) == DBL_ESHAPE);
   for (dbl_shape s : {dbl_shape{1, 1, 65, 8, 8}, dbl_shape{1, 1, 1, (1 << 20) + 8, 8},
                       dbl_shape{1, 1, 1, 8, 1 << 24}, dbl_shape{-1, 1, 1, 8, 8},
@@ -157,7 +161,7 @@ int main(int argc, char** argv) {
                        nullptr) == DBL_ESHAPE);
     CHECK(dbl_workspace_bytes(DBL_OP_HEAD_NLL, s) == bad);
   }
-  CHECK(dbl_workspace_bytes(DBL_OP_HEAD_NLL, dbl_shape{1 << 22, 1 << 10, 1, 8, 8}) == bad);
+  CHECK(dbl_workspace_bytes(DBL_OP_HEAD_NLL, dbl_shape{1 << 14, 1 << 10, 1, 8, 8}) == bad);
   CHECK(g_launches == before);
   // no rows: nothing to do, except dw = 0
   CHECK(dbl_head_nll(dbl_shape{0, 4, 3, 64, 1000}, DBL_BF16, nullptr, P(a(1)), nullptr, nullptr,
@@ -197,7 +201,7 @@ int main(int argc, char** argv) {
   CHECK(dbl_expand_branches_backward(es, P(a(0) + 2), P(a(1)), P(a(2)), P(a(3)), P(a(4)), P(a(5)),
                                      P(a(20)), ews, nullptr) == DBL_EINVAL);
   for (dbl_shape s : {dbl_shape{3, 5, 4, 100, 1}, dbl_shape{3, 5, 65, 96, 1}, dbl_shape{-1, 5, 4, 96, 1},
-                      dbl_shape{3, 5, 64, 1 << 18, 1}, dbl_shape{1 << 22, 1 << 10, 1, 32, 1}})
+                      dbl_shape{3, 5, 64, 1 << 18, 1}, dbl_shape{1 << 14, 1 << 10, 1, 32, 1}})
     CHECK(dbl_expand_branches_backward(s, P(a(0)), P(a(1)), P(a(2)), P(a(3)), P(a(4)), P(a(5)), P(a(20)),
                                        bad, nullptr) == DBL_ESHAPE);
   CHECK(g_launches == before);
@@ -237,6 +241,8 @@ int main(int argc, char** argv) {
     g[0] = nullptr;
     CHECK(dbl_grad_norm(n, g.data(), numel.data(), dt.data(), F(a(0)), P(a(20)), nws, nullptr) == DBL_EINVAL);
     g[0] = keep;
+    CHECK(dbl_grad_norm(n, g.data(), numel.data(), dt.data(), static_cast<float*>(const_cast<void*>(g[1])),
+                        P(a(20)), nws, nullptr) == DBL_EINVAL);  // the norm inside a gradient
     void* okeep = out[1];
     out[1] = const_cast<void*>(g[0]);  // an output over another gradient
     CHECK(dbl_clip_grads(n, g.data(), out.data(), numel.data(), dt.data(), F(a(0)), 1.0f, nullptr) == DBL_EINVAL);

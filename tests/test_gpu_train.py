@@ -201,6 +201,29 @@ def test_a_row_that_is_sure_of_its_token():
         _close(dw, o["dw"], ew, "dw")
 
 
+@pytest.mark.parametrize("case", [("bf16", 3, 72, 300), ("bf16", 50, 200, 3000), ("bf16", 100, 8, 40000),
+                                  ("bf16", 100, 200, 1000), ("bf16", 300, 72, 20500), ("fp32", 5, 70, 300),
+                                  ("fp32", 50, 33, 700)], ids=lambda c: "-".join(map(str, c)))
+def test_an_id_that_an_infinite_weight_rules_out(case):
+    """A logit of minus infinity is a probability of 0 and spoils no other id, wherever the weight stands
+    (also in the first units of a last, partial stage, whose copies are repeated past the end) and however
+    many there are (128 ids in a row are a whole tile)."""
+    from paper_2608_05448_amd import dblast as D
+    dtype, M, d, V = case
+    h, w, x, g = _inputs(dtype, M, 1, 1, d, V, seed=11)
+    unit = (d - 1) // 64 * 64
+    h[..., unit] = h[..., unit].abs() + 0.5
+    keep = torch.ones(V, dtype=torch.bool)
+    keep[3] = keep[128:256] = False
+    x = torch.where(keep[x.long()], x, 4).to(torch.int32)
+    o = _plain(h, w[keep], (keep.cumsum(0) - 1)[x.long()].to(torch.int32), g)
+    w[~keep, unit] = float("-inf")
+    nll, lse = D.dbl_head_nll(h.cuda(), w.cuda(), x.cuda())
+    le, ne = _nll_bounds(o)
+    _close(lse, o["lse"].reshape(lse.shape), le.reshape(lse.shape), "lse")
+    _close(nll, o["nll"].reshape(nll.shape), ne.reshape(nll.shape), "nll")
+
+
 def test_gradient_matches_differences():
     """fp32: central differences of the binary64 loss along random directions."""
     B, K, R, d, V = 2, 3, 2, 24, 90
