@@ -448,7 +448,7 @@ dbl_status dbl_head_nll_backward(dbl_shape shape, int dt, const void* h, const v
  *   shape   B, K, R, d used (V unused); d % 32 == 0, R*d <= 2^23, B*K < 2^24
  *   h       [B, K, d] bf16 trunk states;  W  [R*d, d] bf16;  dout  [B, K, R, d] bf16
  *   dh      out [B, K, d] bf16 or NULL;  dW  out [R*d, d] bf16 or NULL;  dc  out [R*d] bf16 or NULL
- *   ws      workspace of dbl_workspace_bytes(DBL_OP_EXPAND_BACKWARD, shape) bytes (V = 1), needed for dh;
+ *   ws      workspace of dbl_workspace_bytes(DBL_OP_EXPAND_BACKWARD, shape) bytes (V = 1), needed for dh and dW;
  *           otherwise may be 0 and NULL
  * The outputs may overlap neither each other nor an input. B = 0 sets dW and dc to 0.
  * Errors: DBL_EINVAL for null inputs, misaligned pointers or no output; DBL_ESHAPE; DBL_EWORKSPACE.

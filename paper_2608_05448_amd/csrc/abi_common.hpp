@@ -125,20 +125,25 @@ inline WsLayout layout(int op, const dbl_shape& s) {
           const int64_t ids = piece < s.V ? piece : s.V;
           const size_t part =
               sizes[3] * (elem == 2 ? dbl::grad_splits(s.d, M, ids) : dbl::grad_splits_f32(s.d, M, ids));
+          const int splits = dbl::weight_splits(elem == 2, s.d, ids, M);
+          const size_t dw_part = splits > 1 ? static_cast<size_t>(splits) * ids * s.d * sizeof(float) : 0;
           sizes[5] = sizes[5] > grad ? sizes[5] : grad;
           sizes[6] = sizes[6] > part ? sizes[6] : part;
+          sizes[7] = sizes[7] > dw_part ? sizes[7] : dw_part;
         }
-        n = 7;
+        n = 8;
       }
       break;
-    case DBL_OP_EXPAND_BACKWARD:  // the parts of the trunk gradient
+    case DBL_OP_EXPAND_BACKWARD:  // the parts of the trunk gradient and of the weight's
       if (s.B * s.K > dbl::kMaxTrainRows) {
         L.total = SIZE_MAX;
         return L;
       }
       sizes[0] = B * K * static_cast<size_t>(s.d) * sizeof(float) *
                  dbl::grad_splits(s.d, s.B * s.K, s.R * s.d);
-      n = 1;
+      if (const int splits = dbl::weight_splits(true, s.d, s.R * s.d, s.B * s.K); splits > 1)
+        sizes[1] = static_cast<size_t>(splits) * s.R * s.d * s.d * sizeof(float);
+      n = 2;
       break;
     case DBL_OP_GRAD_NORM:  // B tensors
       sizes[0] = static_cast<size_t>(dbl::norm_parts(s.B)) * sizeof(double);

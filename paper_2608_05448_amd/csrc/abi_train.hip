@@ -168,6 +168,8 @@ dbl_status dbl_head_nll_backward(dbl_shape s, int dt, const void* h, const void*
     a.piece = dbl::nll_piece(M, s.V, static_cast<int>(e));
     const int64_t ids = a.piece < s.V ? a.piece : s.V;
     a.splits = a.bf16 ? dbl::grad_splits(s.d, M, ids) : dbl::grad_splits_f32(s.d, M, ids);
+    a.dw_part = reinterpret_cast<float*>(base + L.off[7]);
+    a.dw_splits = dbl::weight_splits(a.bf16, s.d, ids, M);
     return hip_status(dbl::launch_nll_backward(a, static_cast<hipStream_t>(stream)),
                       "head nll backward launch");
   });
@@ -194,12 +196,13 @@ dbl_status dbl_expand_branches_backward(dbl_shape s, const void* h, const void* 
                                {dW, 2 * n * s.d, true}, {dc, 2 * n, true}};
     if (overlapping(spans)) return fail(DBL_EINVAL, "an output overlaps another array");
     dbl::ExpandBackwardArgs a{};
-    if (dh && s.B > 0) {
+    if ((dh || dW) && s.B > 0) {
       WsLayout L;
       dbl_shape sv = s;
       sv.V = 1;
       if (dbl_status st = check_ws(DBL_OP_EXPAND_BACKWARD, sv, ws, ws_bytes, &L)) return st;
       a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.off[0]);
+      a.dW_part = reinterpret_cast<float*>(static_cast<char*>(ws) + L.off[1]);
       a.dh = dh;
     }
     a.P = s.B * s.K;
@@ -211,6 +214,7 @@ dbl_status dbl_expand_branches_backward(dbl_shape s, const void* h, const void* 
     a.dW = dW;
     a.dc = dc;
     a.splits = dbl::grad_splits(s.d, a.P, s.R * s.d);
+    a.dW_splits = dbl::weight_splits(true, s.d, s.R * s.d, a.P);
     return hip_status(dbl::launch_expand_backward(a, static_cast<hipStream_t>(stream)),
                       "expander backward launch");
   });

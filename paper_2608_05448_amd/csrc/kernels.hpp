@@ -195,8 +195,9 @@ struct NllArgs {
   float* tgt;            // workspace [M]
   void* grad;            // workspace [M, piece]
   float* part;           // workspace [splits, M, d]
+  float* dw_part;        // workspace [dw_splits, ids of a piece, d]
   int64_t piece;         // ids per piece, a multiple of 256
-  int splits;
+  int splits, dw_splits;
 };
 
 struct ExpandBackwardArgs {
@@ -209,7 +210,8 @@ struct ExpandBackwardArgs {
   void* dW;              // [R*d, d] or null
   void* dc;              // [R*d] or null
   float* part;           // workspace [splits, P, d]
-  int splits;
+  float* dW_part;        // workspace [dW_splits, R*d, d]
+  int splits, dW_splits;
 };
 
 // One tensor of a set of gradients.
@@ -228,7 +230,8 @@ inline int64_t nll_piece(int64_t M, int64_t V, int elem) {
   const int64_t cap = most < 8192 ? 8192 : most / 4096 * 4096;
   const int64_t pieces = (V + cap - 1) / cap;
   const int64_t each = (V + pieces - 1) / pieces;
-  return (each + 4095) / 4096 * 4096;
+  const int64_t unit = pieces > 1 ? 4096 : 256;
+  return (each + unit - 1) / unit * unit;
 }
 
 // The kernel of a bf16 product [nb, na] over K terms (both: both operands lie across the sum): 256 x 256
@@ -281,6 +284,32 @@ inline int grad_splits_f32(int64_t na, int64_t nb, int64_t K) {
   if (na <= 0 || nb <= 0 || K <= 0) return 1;
   const int64_t s = 768 / (((na + 127) / 128) * ((nb + 63) / 64)), most = (K + 31) / 32;
   return static_cast<int>(s < 1 ? 1 : s < most ? s : most);
+}
+
+// The same for a product with both operands across the sum (the weight gradients): small outputs of many
+// rows would leave most CUs idle. The split with the least time, in ns: whole rounds of 256 workgroups, a
+// stage's time in each and 5 us for its ends; parts written and read at 5 TB/s, and one more launch. One part,
+// and that split, us: 1000 x 512 outputs of 8192 rows 145 and 30; 2048 x 512 of 4096 rows 75 and 29; fp32
+// 2000 x 256 of 8192 rows 380 and 116, 256 x 64 of 2048 rows 97 and 15.
+inline int weight_splits(bool bf16, int64_t na, int64_t nb, int64_t K) {
+  if (na <= 0 || nb <= 0 || K <= 0) return 1;
+  const ProdKind kind = bf16 ? prod_kind(true, na, nb, K) : kProdSmall;
+  if (kind == kProdStream) return 1;
+  const bool pp = kind == kProdPp;
+  const int64_t ta = pp ? 256 : 128, tb = pp ? 256 : bf16 ? 128 : 64, deep = pp ? 64 : 32;
+  const int64_t stage = pp ? 1150 : bf16 ? 470 : 1500;
+  const int64_t tiles = ((na + ta - 1) / ta) * ((nb + tb - 1) / tb), stages = (K + deep - 1) / deep;
+  int best = 1;
+  int64_t least = 0;
+  for (int s = 1; s <= 64 && tiles * s <= 512 && (s == 1 || stages / s >= 4); ++s) {
+    const int64_t t = (tiles * s + 255) / 256 * ((stages + s - 1) / s * stage + 5000) +
+                      (s > 1 ? 4000 + s * na * nb / 625 : 0);
+    if (s == 1 || t < least) {
+      least = t;
+      best = s;
+    }
+  }
+  return best;
 }
 
 constexpr int64_t kMaxThreads = 0xffffffffll;     // of a launch

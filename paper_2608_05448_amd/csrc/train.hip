@@ -199,6 +199,46 @@ __global__ __launch_bounds__(256) void nll_finish_kernel(const NllArgs a, int nT
 }
 
 // ---------------------------------------------------------------------------------------
+// Sum over the splits of four columns of a row's parts, eight loads in flight.
+__device__ __forceinline__ f32x4 sum_parts(const float* part, int64_t stride, int splits) {
+  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  int s = 0;
+  for (; s + 8 <= splits; s += 8) {
+    f32x4 u[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const f32x4u*>(part + (s + i) * stride);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v += u[i];
+  }
+  for (; s < splits; ++s) v += *reinterpret_cast<const f32x4u*>(part + s * stride);
+  return v;
+}
+__device__ __forceinline__ void store4(__bf16* o, f32x4 v) {
+  *reinterpret_cast<bf16x4*>(o) = bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]),
+                                         static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
+}
+
+// A weight gradient from its parts, n values each.
+template <class T>
+__global__ __launch_bounds__(256) void weight_finish_kernel(const float* __restrict__ part, int64_t n, int splits,
+                                                            T* __restrict__ out) {
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 1024 + 4 * threadIdx.x;
+  if (i + 4 <= n) {
+    const f32x4 v = sum_parts(part + i, n, splits);
+    if constexpr (sizeof(T) == 2)
+      store4(out + i, v);
+    else
+      *reinterpret_cast<f32x4*>(out + i) = v;
+  } else {
+    for (int64_t j = i; j < n; ++j) {
+      float v = 0.0f;
+      for (int s = 0; s < splits; ++s) v += part[s * n + j];
+      out[j] = static_cast<T>(v);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------
 // bf16 products out[b, a] = sum_k B(k, b) A[k, a] with A [K, lda] row-major.
 
 struct Prod {
@@ -980,8 +1020,9 @@ hipError_t launch_prod_out(Prod p, hipStream_t stream) {
     return hipGetLastError();
   }
   if constexpr (TRB) {
-    if (kind == kProdStream)
-      return p.K <= 128 ? launch_stream<2, OUT>(p, stream) : launch_stream<4, OUT>(p, stream);
+    if constexpr (OUT != kOutPart)
+      if (kind == kProdStream)
+        return p.K <= 128 ? launch_stream<2, OUT>(p, stream) : launch_stream<4, OUT>(p, stream);
     return launch_ring<RingShort, TRB, OUT>(p, stream);
   } else {
     if (kind == kProdFew)
@@ -997,10 +1038,23 @@ hipError_t launch_prod_part(const Prod& p, hipStream_t stream) {
   return launch_prod_out<false, kOutPart>(p, stream);
 }
 
+// A product of two operands across the sum in parts, and their sum.
+template <class T, class A, class F>
+hipError_t launch_weight_parts(A p, T* out, hipStream_t stream, F launch) {
+  p.part_stride = p.na * p.nb;
+  const hipError_t e = launch(p, stream);
+  if (e != hipSuccess) return e;
+  const int64_t blocks = (p.part_stride + 1023) / 1024;  // of at most 512 tiles
+  hipLaunchKernelGGL(weight_finish_kernel<T>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, p.part,
+                     p.part_stride, p.splits, out);
+  return hipGetLastError();
+}
+
 // The bf16 product of two operands across the sum. An output that would fill the 256 MB Infinity Cache is
 // written past it (151936 x 2560 outputs of 60 terms 174 ->
 // 141 us); a smaller one stays there for its next reader (50257 x 1000 outputs 34 us, 43 non-temporally).
 hipError_t launch_prod(const Prod& p, hipStream_t stream) {
+  if (p.splits > 1) return launch_weight_parts<__bf16>(p, p.out, stream, launch_prod_out<true, kOutPart>);
   return 2 * p.na * p.nb >= (int64_t(256) << 20) ? launch_prod_out<true, kOutStream>(p, stream)
                                                 : launch_prod_out<true, kOutKeep>(p, stream);
 }
@@ -1255,26 +1309,6 @@ hipError_t launch_f32(const F32Args& p, hipStream_t stream) {
   return launch_f32_rows<TRA, TRB, EPI, 64>(p, stream);
 }
 
-// ---------------------------------------------------------------------------------------
-// Sum over the splits of four columns of a row's parts, eight loads in flight.
-__device__ __forceinline__ f32x4 sum_parts(const float* part, int64_t stride, int splits) {
-  f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  int s = 0;
-  for (; s + 8 <= splits; s += 8) {
-    f32x4 u[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) u[i] = *reinterpret_cast<const f32x4u*>(part + (s + i) * stride);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v += u[i];
-  }
-  for (; s < splits; ++s) v += *reinterpret_cast<const f32x4u*>(part + s * stride);
-  return v;
-}
-__device__ __forceinline__ void store4(__bf16* o, f32x4 v) {
-  *reinterpret_cast<bf16x4*>(o) = bf16x4{static_cast<__bf16>(v[0]), static_cast<__bf16>(v[1]),
-                                         static_cast<__bf16>(v[2]), static_cast<__bf16>(v[3])};
-}
-
 // dh of every row: the sum of its parts times its scale, 0 for the rows that do not count. A wave takes
 // 256 columns of a row.
 template <class T>
@@ -1401,8 +1435,9 @@ hipError_t nll_piece_bf16(const NllArgs& a, int64_t v0, int64_t n, hipStream_t s
   q.nb = n;
   q.K = M;
   q.count = M > 0 ? a.count : nullptr;
+  q.part = a.dw_part;
   q.out = static_cast<__bf16*>(a.dw) + v0 * a.d;
-  q.splits = 1;
+  q.splits = a.dw_splits;
   return launch_prod(q, stream);
 }
 
@@ -1448,8 +1483,10 @@ hipError_t nll_piece_f32(const NllArgs& a, int64_t v0, int64_t n, hipStream_t st
   r.nb = n;
   r.K = M;
   r.count_k = M > 0 ? a.count : nullptr;
+  r.part = a.dw_part;
   r.out = static_cast<float*>(a.dw) + v0 * a.d;
-  r.splits = 1;
+  r.splits = a.dw_splits;
+  if (r.splits > 1) return launch_weight_parts<float>(r, r.out, stream, launch_f32<true, true, kF32Part>);
   return launch_f32<true, true, kF32Out>(r, stream);
 }
 
@@ -1538,8 +1575,9 @@ hipError_t launch_expand_backward(const ExpandBackwardArgs& a, hipStream_t strea
     q.ldb = n;
     q.nb = n;
     q.K = a.P;
+    q.part = a.dW_part;
     q.out = static_cast<__bf16*>(a.dW);
-    q.splits = 1;
+    q.splits = a.dW_splits;
     e = launch_prod(q, stream);
     if (e != hipSuccess) return e;
   }

@@ -512,12 +512,13 @@ def dbl_expand_branches_backward(h, W, dout, want_dh=True, want_dW=True, want_dc
     if want_dh or dh is not None:
         dh = torch.empty_like(h) if dh is None else dh
         _need(dh, "dh", torch.bfloat16, (B, K, d))
-        ws, nws = _workspace(DBL_OP_EXPAND_BACKWARD, shape, dev, ws)
-    else:
-        ws, nws = None, 0
     if want_dW or dW is not None:
         dW = torch.empty_like(W) if dW is None else dW
         _need(dW, "dW", torch.bfloat16, (R * d, d))
+    if dh is not None or dW is not None:
+        ws, nws = _workspace(DBL_OP_EXPAND_BACKWARD, shape, dev, ws)
+    else:
+        ws, nws = None, 0
     if want_dc or dc is not None:
         dc = W.new_empty(R * d) if dc is None else dc
         _need(dc, "dc", torch.bfloat16, (R * d,))

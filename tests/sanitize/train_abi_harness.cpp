@@ -6,6 +6,7 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <cmath>
 #include <limits>
 #include <vector>
@@ -112,7 +113,10 @@ int main(int argc, char** argv) {
              {g_nll.hc, e * M * s.d},
              {g_nll.hs, e * M * s.d},
              {g_nll.grad, e * M * g_nll.piece},
-             {g_nll.part, 4 * M * s.d * g_nll.splits}}, bws);
+             {g_nll.part, 4 * M * s.d * g_nll.splits},
+             {g_nll.dw_part, g_nll.dw_splits > 1 ? 4 * std::min<size_t>(g_nll.piece, s.V) * s.d *
+                                                       g_nll.dw_splits : 0}}, bws);
+      CHECK(g_nll.dw_splits >= 1);
       CHECK(dbl_head_nll_backward(s, dt, P(a(0)), P(a(1)), I(a(2)), F(a(3)), F(a(4)), F(a(5)),
                                   P(a(6)), nullptr, P(a(20)), bws, nullptr) == DBL_OK);
       CHECK(!g_nll.dw && !g_nll.hs);
@@ -186,7 +190,7 @@ int main(int argc, char** argv) {
                                      P(a(20)), ews, nullptr) == DBL_OK);
   CHECK(g_expand.P == 15 && g_expand.R == 4 && g_expand.d == 96 && g_expand.part == P(a(20)) &&
         g_expand.splits >= 1 && ews >= static_cast<size_t>(g_expand.splits) * 15 * 96 * 4);
-  CHECK(dbl_expand_branches_backward(es, P(a(0)), P(a(1)), P(a(2)), nullptr, P(a(4)), nullptr, nullptr, 0,
+  CHECK(dbl_expand_branches_backward(es, P(a(0)), P(a(1)), P(a(2)), nullptr, P(a(4)), nullptr, P(a(20)), ews,
                                      nullptr) == DBL_OK);
   CHECK(!g_expand.dh && !g_expand.dc && g_expand.dW);
   before = g_launches;
@@ -200,6 +204,21 @@ int main(int argc, char** argv) {
                                      ews, nullptr) == DBL_EINVAL);
   CHECK(dbl_expand_branches_backward(es, P(a(0) + 2), P(a(1)), P(a(2)), P(a(3)), P(a(4)), P(a(5)),
                                      P(a(20)), ews, nullptr) == DBL_EINVAL);
+  CHECK(dbl_expand_branches_backward(es, P(a(0)), P(a(1)), P(a(2)), nullptr, P(a(4)), nullptr, nullptr, 0,
+                                     nullptr) == DBL_EWORKSPACE);
+  CHECK(g_launches == before);
+  CHECK(dbl_expand_branches_backward(es, P(a(0)), P(a(1)), P(a(2)), nullptr, nullptr, P(a(5)), nullptr, 0,
+                                     nullptr) == DBL_OK);
+  dbl_shape ms{256, 16, 4, 512, 1};  // a small weight gradient of many rows, in parts
+  const size_t mws = dbl_workspace_bytes(DBL_OP_EXPAND_BACKWARD, ms);
+  CHECK(dbl_expand_branches_backward(ms, P(a(0)), P(a(1)), P(a(2)), P(a(3)), P(a(4)), P(a(5)), P(a(20)), mws,
+                                     nullptr) == DBL_OK);
+  CHECK(g_expand.dW_splits > 1 &&
+        reinterpret_cast<uintptr_t>(g_expand.dW_part) >=
+            a(20) + static_cast<size_t>(g_expand.splits) * 4096 * 512 * 4 &&
+        reinterpret_cast<uintptr_t>(g_expand.dW_part) + static_cast<size_t>(g_expand.dW_splits) * 4 * 512 * 512 * 4 <=
+            a(20) + mws);
+  before = g_launches;
   for (dbl_shape s : {dbl_shape{3, 5, 4, 100, 1}, dbl_shape{3, 5, 65, 96, 1}, dbl_shape{-1, 5, 4, 96, 1},
                       dbl_shape{3, 5, 64, 1 << 18, 1}, dbl_shape{1 << 14, 1 << 10, 1, 32, 1}})
     CHECK(dbl_expand_branches_backward(s, P(a(0)), P(a(1)), P(a(2)), P(a(3)), P(a(4)), P(a(5)), P(a(20)),

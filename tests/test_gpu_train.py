@@ -158,6 +158,15 @@ HEAD_CASES = [
     ("bf16", 2, 50, 1, 136, 42000, "some"),
     ("fp32", 1, 31, 1, 63, 95, "none"), ("fp32", 1, 33, 1, 65, 97, "none"),
     ("fp32", 2, 64, 3, 250, 3001, "some"),      # sums in several parts
+    ("bf16", 64, 16, 1, 200, 300, "some"),      # many rows and a small head: dw in parts as well, of 256 x 256
+    ("bf16", 64, 16, 2, 264, 700, "first"),     # tiles (most of them and all but one of the rows gone),
+    ("bf16", 64, 16, 1, 256, 256, "but-last"),
+    ("bf16", 64, 16, 1, 256, 257, "all"),
+    ("bf16", 37, 15, 2, 64, 1000, "some"),      # of 128 x 128 tiles,
+    ("bf16", 41, 13, 3, 520, 77, "some"),
+    ("fp32", 37, 11, 2, 33, 77, "some"),        # and in fp32, also where a part's length is odd
+    ("fp32", 64, 16, 1, 131, 259, "some"),
+    ("fp32", 64, 16, 1, 5, 3, "but-last"),
 ]
 
 
@@ -312,6 +321,7 @@ EXPAND_CASES = [
     # 2^26 weights: the weight gradient's stream kernel with 65, 128, 201 and 256 rows, whole and partial
     # panels of 512 columns
     (1, 65, 9, 2752), (1, 128, 16, 2080), (3, 67, 8, 2912), (1, 256, 4, 4096),
+    (64, 16, 2, 256), (43, 13, 4, 512), (70, 15, 1, 96), (300, 7, 3, 32),  # small weights of many rows: in parts
 ]
 
 
