@@ -223,7 +223,7 @@ struct GradTensor {
 };
 
 // Ids of the vocabulary that the head's backward pass takes at a time: as many as give a gradient of
-// about 1 GiB, at least 8192, in equal pieces of a multiple of 4096.
+// about 1 GiB, at least 8192, in equal pieces of a multiple of 4096 (a single piece: of 256).
 constexpr int64_t kPieceBytes = int64_t(1) << 30;
 inline int64_t nll_piece(int64_t M, int64_t V, int elem) {
   const int64_t most = kPieceBytes / (elem * (M > 0 ? M : 1));

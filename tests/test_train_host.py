@@ -56,6 +56,10 @@ def test_workspaces_grow_with_the_pieces_not_with_the_vocabulary():
         # loss alone: 4 bytes for every 32 ids of a row at most
         f = D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL, rows, 1, 1, d, V)
         assert f <= rows * (V // 8 + 8 + 4 * d + 64) + 2048
+    # a small vocabulary is not padded to a piece
+    rows, small = 1 << 20, 200
+    n = D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL_BACKWARD, rows, 1, 1, d, small)
+    assert n <= rows * (256 * 4 + 2 * 4 * d + 16 + 4) + rows * d * 4 + 64 * small * d * 4 + 4096
     assert D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL_BACKWARD, 0, 1, 1, d, V) >= 0
     assert D.dbl_workspace_bytes(15, 1, 1, 1, 8, 8) == ctypes.c_size_t(-1).value
     assert D.dbl_workspace_bytes(20, 1, 1, 1, 8, 8) == ctypes.c_size_t(-1).value
