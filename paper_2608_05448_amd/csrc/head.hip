@@ -383,15 +383,63 @@ __device__ __forceinline__ void tile_nll_store(f32x16 (&acc)[NRB][NCB], const Ep
   }
 }
 
+// The same where two waves share a tile, 64 ids each (id 64 wv + ... of the tile), in the same order of
+// additions: the second wave takes the first one's sum on. xc: 64 floats of LDS for the two.
+template <int NRB, int NCB>
+__device__ __forceinline__ void pair_nll_store(f32x16 (&acc)[NRB][NCB], const EpiArgs& e, int64_t M,
+                                               int64_t V, int64_t v0w, int64_t m0w, int lane, int wv,
+                                               float* xc) {
+  static_assert(NRB == 2 && NCB == 1, "half a tile");
+  const int half = lane >> 5;
+  const int64_t rest = V - v0w - 4 * half;
+  const int lim = static_cast<int>(rest < 64 ? rest : 64);
+  const int64_t m = m0w + (lane & 31);
+  float x[32];
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    x[i] = 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) < lim ? acc[i >> 4][0][i & 15] : -INFINITY;
+  const int64_t o = m < M ? e.rows[m].token - v0w - 4 * half : -1;
+  if (o >= 0 && o < lim && !(o & 4)) {
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) t = o == 32 * (i >> 4) + 8 * ((i & 15) >> 2) + (i & 3) ? x[i] : t;
+    e.tgt[m] = t;
+  }
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) mx = fmaxf(mx, x[i]);
+  mx = fmaxf(mx, __shfl_xor(mx, 32));
+  if (half == wv) xc[32 * wv + (lane & 31)] = mx;
+  __syncthreads();
+  mx = fmaxf(mx, xc[32 * (wv ^ 1) + (lane & 31)]);
+  __syncthreads();
+  const float nb = mx > -INFINITY ? -mx * kLog2e : 0.0f;
+  float s = 0.0f;
+  if (wv == 0) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, nb));
+    xc[lane] = s;
+  }
+  __syncthreads();
+  if (wv == 1) {
+    s = xc[lane];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) s += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, nb));
+    s += __shfl_xor(s, 32);
+    if (m < M && half == 0) e.lmass[m * e.nT + v0w / kVTile] = mx + __logf(s);
+  }
+}
+
 // Epilogue of dbl_head_nll_backward: the logits' gradient of a row over its scale, in bf16 (see
 // TrainRow): exp(logit - lse) / q for every id but the token, -1 for the token; 0 for the ids of a tile past V. 32 rows
-// x 128 ids at a time go through xp (8 KB of LDS of this wave), so that a store instruction writes four
-// whole 256-byte row segments (16-byte chunk c of row r at chunk c ^ (r % 16)).
+// x 32 NRB ids at a time go through xp (2 NRB KB of LDS of this wave), so that a store instruction writes
+// whole row segments of 64 NRB bytes (16-byte chunk c of row r at chunk c ^ (r % (4 NRB))).
 template <int NRB, int NCB>
 __device__ __forceinline__ void tile_grad_store(f32x16 (&acc)[NRB][NCB], const EpiArgs& e, int64_t M,
                                                 int64_t V, int64_t v0w, int64_t m0w, int lane,
                                                 char* xp) {
   typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  constexpr int ROWB = 64 * NRB, CH = 4 * NRB, RPI = 64 / CH;  // a row's bytes and chunks; rows an instruction
   const int half = lane >> 5;
   const int lr = lane & 31;
   const int lim = static_cast<int>(V - v0w < kVTile ? V - v0w : kVTile) - 4 * half;
@@ -414,18 +462,18 @@ __device__ __forceinline__ void tile_grad_store(f32x16 (&acc)[NRB][NCB], const E
           p = o == at ? row.at_token : p;
           y[q] = static_cast<__bf16>(at < lim ? p : 0.0f);
         }
-        *reinterpret_cast<bf16x4*>(xp + lr * 256 + (((rb * 4 + g) ^ (lr & 15)) * 16) + half * 8) = y;
+        *reinterpret_cast<bf16x4*>(xp + lr * ROWB + (((rb * 4 + g) ^ (lr & (CH - 1))) * 16) + half * 8) = y;
       }
     // Wave-private LDS region: the writes above precede these reads in the wave's LDS queue.
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 #pragma unroll
-    for (int jj = 0; jj < 8; ++jj) {
-      const int rr = 4 * jj + (lane >> 4);
+    for (int jj = 0; jj < 32 / RPI; ++jj) {
+      const int rr = RPI * jj + lane / CH;
       const u32x4 y =
-          *reinterpret_cast<const u32x4*>(xp + rr * 256 + (((lane & 15) ^ (rr & 15)) * 16));
+          *reinterpret_cast<const u32x4*>(xp + rr * ROWB + (((lane & (CH - 1)) ^ (rr & (CH - 1))) * 16));
       const int64_t mm = m0w + cb * 32 + rr;
-      if (mm < M) *reinterpret_cast<u32x4*>(grad + mm * e.ldg + v0w + 8 * (lane & 15)) = y;
+      if (mm < M) *reinterpret_cast<u32x4*>(grad + mm * e.ldg + v0w + 8 * (lane & (CH - 1))) = y;
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
@@ -1576,14 +1624,19 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void head_bf16_few_ker
   asm volatile("" ::: "memory");
 
   const int64_t v0w = v0 + wv * C::TV;
+  if constexpr (EPI == kEpiNll && C::TV == 64) {
+    pair_nll_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, wv & 1,
+                             reinterpret_cast<float*>(smem) + 64 * (wv / 2 * C::WM + wm));
+    return;
+  }
   if (v0w >= V) return;
   if constexpr (EPI == kEpiExpand) {
     expand_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
   } else if constexpr (EPI == kEpiNll) {
     tile_nll_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane);
   } else if constexpr (EPI == kEpiGrad) {
-    static_assert(C::NW * 8192 <= C::kLds, "8 KB of the ring per wave that stores");
-    tile_grad_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * 8192);
+    static_assert(C::NW * NRB * 2048 <= C::kLds, "2 NRB KB of the ring per wave that stores");
+    tile_grad_store<NRB, NCB>(acc, ea, M, V, v0w, m0 + wm * C::TM, lane, smem + wave * NRB * 2048);
   } else {
     static_assert(C::TV == kVTile && C::WV * C::WM * 16384 <= C::kLds,
                   "head epilogue: 16 KB of the ring per wave that stores");
@@ -1803,7 +1856,12 @@ constexpr int64_t kFewRows = 128;
 // the next smaller tiles are taken (us, rows x ids, d, by tile: 256 x 256, 256 x 128, 128 x 128 ids x rows:
 // 320 x 6706, 2560: 49, 40, 33; 978 x 3456, 2560: 49, 47, 34; 460 x 14360, 2048: 44, 38, 51; 1079 x 6264,
 // 4096: 78, 69, 94; 600 x 20000, 1024, 237 of the largest: 32, 41, 57).
-using HeadFew128Short = FewCfg<128, 128, 1, 4, 1, 4>;
+// Tiles of 128 ids are bound by what a wave issues in a stage, so twice the waves share them, 64 ids each (us,
+// waves of 128 ids and of 64: 16 rows x 14520, 4096: 43.5, 35; 60 x 32000, 4096: 47, 43; 60 x 1000, 4096: 41, 31;
+// 32 x 26564, 2560: 32, 29; 120 x 1000, 4096: 42, 37; deeper rings 0 to 5%); tiles of 256 ids are bound by the
+// weight's stream, and gain nothing (60 x 50257, 4096: 66, 68).
+using HeadPair64 = FewCfg<128, 64, 2, 2, 1, 3>;
+using HeadPair128 = FewCfg<128, 128, 2, 4, 1, 4>;
 inline bool few_tiles(int64_t V, int64_t M, int bv, int bm) {
   return ((V + bv - 1) / bv) * ((M + bm - 1) / bm) < kFewTiles;
 }
@@ -1813,12 +1871,15 @@ hipError_t launch_head_few(const __bf16* h, const __bf16* w, const EpiArgs& ea, 
   if (M > HeadFew64::BM) {
     if constexpr (epi_train(EPI))
       if (few_tiles(V, M, HeadFew128::BV, HeadFew128::BM))
-        return launch_few<HeadFew128Short, EPI, TAIL>(h, w, ea, M, V, d, stream);
+        return launch_few<HeadPair128, EPI, TAIL>(h, w, ea, M, V, d, stream);
     return launch_few<HeadFew128, EPI, TAIL>(h, w, ea, M, V, d, stream);
   }
   if ((V + HeadFew64::BV - 1) / HeadFew64::BV >= kFewTiles)
     return launch_few<HeadFew64, EPI, TAIL>(h, w, ea, M, V, d, stream);
-  return launch_few<HeadFew64Short, EPI, TAIL>(h, w, ea, M, V, d, stream);
+  if constexpr (epi_train(EPI))
+    return launch_few<HeadPair64, EPI, TAIL>(h, w, ea, M, V, d, stream);
+  else
+    return launch_few<HeadFew64Short, EPI, TAIL>(h, w, ea, M, V, d, stream);
 }
 
 // The head's GEMM with the kernel that its shape takes. The training epilogues have no kernels of their
