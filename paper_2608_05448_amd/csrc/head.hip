@@ -1287,6 +1287,7 @@ __device__ __forceinline__ void pp_barrier() {
 
 // TAIL: d % 8 == 0 only. The last stage holds `last` < 64 units: chunks past them fetch the row's first
 // chunk of the stage, and count as 0 in both operands' fragments (what they repeat may be infinite).
+// The partial stage is the last one that is walked: walk_start is 0 for such d.
 template <int EPI, bool TAIL = false>
 __global__ __launch_bounds__(512, 1) void head_bf16_pp_kernel(
     const __bf16* __restrict__ h, const __bf16* __restrict__ w, const EpiArgs ea, int64_t M,
