@@ -407,7 +407,8 @@ dbl_status dbl_early_determinism(int64_t M, int64_t b, int64_t V, const int32_t*
  *     nll[b, k, z] = lse[b, k, z] - logit[b, k, z, x[b, k]].
  * A position whose token is outside [0, V) (padding, positions that are not trained on) does not
  * count: its nll and lse are 0, its states are not looked at (they may hold anything) and it costs
- * next to nothing. A row's results do not depend on the other rows of the call.
+ * next to nothing. A row's results do not depend on the other rows of the call. A row that counts and has a
+ * logit of NaN or plus infinity gets NaN for both (minus infinity is a probability of 0).
  *   dt    DBL_BF16 (d % 8 == 0) or DBL_F32
  *   h     [B, K, R, d] branch states;  w  [V, d] head weight, both of type dt
  *   x     [B, K] int32 tokens

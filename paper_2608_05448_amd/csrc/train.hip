@@ -155,7 +155,8 @@ hipError_t gather_rows(const NllArgs& a, hipStream_t stream) {
 
 // lse and nll of every row from the tile log-masses; 0 for the rows that do not count. One wave a row,
 // 32 masses a lane at a time (V up to 262,144 in one pass): all loads in flight, then their maximum and
-// their sum of exponentials, joined to the running ones.
+// their sum of exponentials, joined to the running ones. A tile with a NaN or a logit of plus infinity has a
+// mass of NaN (exp(inf - inf)), and so have the row's lse and nll.
 __global__ __launch_bounds__(256) void nll_finish_kernel(const NllArgs a, int nT) {
   constexpr int kRegs = 32;
   const int64_t m = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
@@ -178,12 +179,13 @@ __global__ __launch_bounds__(256) void nll_finish_kernel(const NllArgs a, int nT
       for (int k = 0; k < kRegs; ++k) top = fmaxf(top, v[k]);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+      // Masses of minus infinity only add 0. So that a NaN, which the maximum passes over, is added all the
+      // same where it leaves none, the exponentials are taken there as well.
+      const float base = top > -INFINITY ? top : 0.0f;
+      if (top > -INFINITY) s *= expf(mx - top);
       float add = 0.0f;
-      if (top > -INFINITY) {
-        s *= expf(mx - top);
 #pragma unroll
-        for (int k = 0; k < kRegs; ++k) add += expf(v[k] - top);
-      }
+      for (int k = 0; k < kRegs; ++k) add += expf(v[k] - base);
       s += add;
       mx = top;
     }
