@@ -102,10 +102,10 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const NllArgs a, int c
   const int64_t from = p * R + r, to = static_cast<int64_t>(at) * R + r;
   TrainRow row{0.0f, 0.0f, 0.0f, token};
   if (a.g) {
-    const float lse = a.lse[from], g = a.g[from];
-    const float q = -expm1f(-fmaxf(a.nll[from], 0.0f));
+    const float lse = a.lse[from], g = a.g[from], nll = a.nll[from];
+    const float q = nll < 0.0f ? 0.0f : -expm1f(-nll);  // NaN stays, also in qc (fmaxf would drop it)
     if (sizeof(T) == 2) {
-      const float qc = fmaxf(q, 0x1p-24f);
+      const float qc = q < 0x1p-24f ? 0x1p-24f : q;
       row.shift = (lse + logf(qc)) * kLog2e;
       row.at_token = -q / qc;
       row.scale = g * qc;

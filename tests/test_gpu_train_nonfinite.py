@@ -89,3 +89,36 @@ def test_rows_of_minus_infinity_and_certain_rows_are_as_they_were(dtype):
     x.zero_()
     nll, lse = D.dbl_head_nll(h, w1, x)
     assert (nll == 0).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_gradients_of_a_row_that_is_not_a_number(case):
+    """Its states' gradient is NaN in every unit, and so is every weight's, the token's own among them (each
+    is a sum over the rows that count); the other rows' gradients are those of the clean call."""
+    from paper_2608_05448_amd import dblast as D
+    print(f"[nonfinite] gradient {case}", flush=True)
+    h, w, x, g = _inputs(*case)
+    M, d = h.shape[0], h.shape[3]
+    nll, lse = D.dbl_head_nll(h, w, x)
+    clean, _ = D.dbl_head_nll_backward(h, w, x, nll, lse, g)
+    row = M // 2
+    h[row, 0, 0, d - 1] = NAN
+    nll, lse = D.dbl_head_nll(h, w, x)
+    dh, dw = D.dbl_head_nll_backward(h, w, x, nll, lse, g)
+    others = torch.arange(M, device="cuda") != row
+    assert torch.equal(dh[others], clean[others])
+    assert torch.isnan(dh[row]).all()
+    assert torch.isnan(dw).all(), torch.nonzero(~torch.isnan(dw).all(1))[:4]
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_gradients_of_a_vocabulary_of_one_id(dtype):
+    """The token is the only id: its entry is all there is to show a NaN in."""
+    from paper_2608_05448_amd import dblast as D
+    h, w, x, g = _inputs(dtype, 3, 64, 1)
+    h[1, 0, 0, 9] = NAN
+    nll, lse = D.dbl_head_nll(h, w, x)
+    assert torch.isnan(nll[1]).all() and (nll[[0, 2]] == 0).all()
+    dh, dw = D.dbl_head_nll_backward(h, w, x, nll, lse, g)
+    assert torch.isnan(dh[1]).all() and torch.isnan(dw).all()
+    assert (dh[[0, 2]] == 0).all()
