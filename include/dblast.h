@@ -479,13 +479,14 @@ dbl_status dbl_grad_norm(int64_t n, const void* const* grads, const int64_t* num
 /*
  * dbl_clip_grads - gradients scaled to a largest global norm:
  *     out[i][j] = grads[i][j] * min(1, max_norm / (norm + 1e-6)),
- * computed in fp32 and rounded once. A norm that is not finite (an infinity or NaN among the gradients)
- * is not hidden: an infinite one scales by 0, a NaN one gives NaN everywhere.
+ * computed in fp32 and rounded once. A norm that is not finite (an infinity or NaN among the gradients, or
+ * finite ones whose norm is past fp32) is not hidden: under a finite max_norm an infinite one scales by 0, and
+ * a NaN one gives NaN everywhere under any.
  *   n, grads, numel, dt   as dbl_grad_norm
  *   out       [n] device pointers of the same types and sizes, or NULL: in place. out[i] is grads[i] or
  *             overlaps no gradient and no other output
  *   norm      one fp32 (device), for example dbl_grad_norm's (of several devices' parts together)
- *   max_norm  >= 0 (infinity: no limit)
+ *   max_norm  >= 0 (infinity: no limit, the scale is 1 unless the norm is NaN)
  * Errors: as dbl_grad_norm, and DBL_EINVAL for overlapping tensors or max_norm < 0 or NaN.
  */
 dbl_status dbl_clip_grads(int64_t n, const void* const* grads, void* const* out,

@@ -128,7 +128,9 @@ __global__ __launch_bounds__(256) void norm_finish_kernel(const double* __restri
 // themselves, which a scale of 1 leaves alone.
 __global__ __launch_bounds__(256) void clip_kernel(const ClipSet s, int count, int chunks, int same,
                                                    const float* __restrict__ norm, float max_norm) {
-  const float ratio = max_norm / (*norm + 1e-6f);
+  const float value = *norm;
+  // No limit scales by 1 under an infinite norm too, where the quotient would be inf / inf.
+  const float ratio = max_norm == INFINITY && value == value ? 1.0f : max_norm / (value + 1e-6f);
   const float scale = ratio > 1.0f ? 1.0f : ratio;  // NaN stays
   if (same && scale == 1.0f) return;
   const int tid = threadIdx.x;
