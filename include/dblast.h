@@ -434,7 +434,9 @@ dbl_status dbl_head_nll(dbl_shape shape, int dt, const void* h, const void* w, c
  *   dh    out [B, K, R, d] of type dt;  dw  out [V, d] of type dt, or NULL (the head is frozen)
  *   ws    workspace of dbl_workspace_bytes(DBL_OP_HEAD_NLL_BACKWARD, shape) bytes (a piece of the
  *         logits' gradient, up to about 1 GiB or, if that is more, of 8192 ids; copies of h; and
- *         fp32 sums of dh and, for a small head and many rows, of dw)
+ *         fp32 sums of dh, in as many parts as it takes to fill the GPU (60 rows at d = 2560: 38, 2048 at
+ *         d = 4096: 2, 8192: 1), and, for a small head and many rows, of dw). The size serves either type:
+ *         bf16 calls need less of it than fp32 ones
  * dh and dw may overlap neither each other nor an input. Errors: as dbl_head_nll.
  */
 dbl_status dbl_head_nll_backward(dbl_shape shape, int dt, const void* h, const void* w,

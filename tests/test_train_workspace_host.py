@@ -1,0 +1,54 @@
+"""Workspaces of the training operators, on the host: what dbl_workspace_bytes answers for them, part by
+part, and what the binding takes as a workspace."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2608_05448_amd import dblast as D
+
+SIZE_MAX = ctypes.c_size_t(-1).value
+
+
+def _up(n, to):
+    return -(-n // to) * to
+
+
+def _piece(rows, V, elem):
+    """Ids that the gradient takes at a time, as the header has it: about 1 GiB of the logits' gradient, at
+    least 8192 ids, in equal pieces of a multiple of 4096 (256 for one)."""
+    cap = max(8192, (1 << 30) // (elem * rows) // 4096 * 4096)
+    pieces = -(-V // cap)
+    return _up(-(-V // pieces), 4096 if pieces > 1 else 256)
+
+
+# rows, d, V, copies of dh in fp32, sums of dw in parts (of a piece's ids)
+PARTS = [
+    (8, 64, 256, 8, 0),              # fp32 parts of 32 terms; one part for the weight
+    (60, 2560, 151936, 38, 0),       # fp32: 768 workgroups over 20 tiles; bf16: 256 over 10 (25 parts)
+    (256, 64, 151936, 256, 0),       # 128 x 128 tiles: 512 workgroups over 2
+    (2048, 64, 151936, 32, 0),
+    (8192, 64, 151936, 8, 0),
+    (32768, 64, 151936, 2, 4),       # pieces of 8192 ids: their weights in 4 parts (fp32)
+    (2048, 4096, 151936, 2, 0),      # 128 tiles of 256 x 256 on 256 CUs: two parts
+    (8192, 4096, 151936, 1, 0),
+    (65536, 4096, 151936, 1, 0),
+]
+
+
+@pytest.mark.parametrize("case", PARTS, ids=str)
+def test_gradient_workspace_part_by_part(case):
+    rows, d, V, dh, dw = case
+    grad = max(rows * _piece(rows, V, e) * e for e in (2, 4))
+    ids = min(V, _piece(rows, V, 4))
+    parts = [4, 4 * rows, 16 * rows, 4 * rows * d, 4 * rows * d, grad, 4 * rows * d * dh, 4 * ids * d * dw]
+    want = sum(_up(n, 256) for n in parts)
+    assert D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL_BACKWARD, rows, 1, 1, d, V) == want, \
+        (D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL_BACKWARD, rows, 1, 1, d, V) - want) / (4 * rows * d)
+
+
+@pytest.mark.parametrize("rows", [1, 60, 2048, 65536])
+def test_loss_workspace_part_by_part(rows):
+    d, V = 4096, 151936
+    parts = [4, 4 * rows, 16 * rows, 4 * rows * d, 4 * rows * (V // 32), 4 * rows]
+    assert D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL, rows, 1, 1, d, V) == sum(_up(n, 256) for n in parts)
