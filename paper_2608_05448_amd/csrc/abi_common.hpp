@@ -146,6 +146,10 @@ inline WsLayout layout(int op, const dbl_shape& s) {
       n = 2;
       break;
     case DBL_OP_GRAD_NORM:  // B tensors
+      if (s.B > dbl::kMaxTensors) {
+        L.total = SIZE_MAX;
+        return L;
+      }
       sizes[0] = static_cast<size_t>(dbl::norm_parts(s.B)) * sizeof(double);
       n = 1;
       break;

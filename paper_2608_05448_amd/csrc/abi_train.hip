@@ -69,7 +69,7 @@ dbl::NllArgs nll_args(const dbl_shape& s, int dt, const void* h, const void* w, 
 dbl_status check_tensors(int64_t n, const void* const* grads, const int64_t* numel,
                          const int32_t* dt, void* const* out, bool clip,
                          std::vector<dbl::GradTensor>* to) {
-  if (n < 0 || n > (int64_t(1) << 20)) return fail(DBL_ESHAPE, "need 0 <= n <= 2^20 tensors");
+  if (n < 0 || n > dbl::kMaxTensors) return fail(DBL_ESHAPE, "need 0 <= n <= 2^20 tensors");
   if (n > 0 && (!grads || !numel || !dt)) return fail(DBL_EINVAL, "NULL array");
   to->resize(static_cast<size_t>(n));
   int64_t all = 0;

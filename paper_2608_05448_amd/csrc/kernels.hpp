@@ -315,6 +315,7 @@ inline int weight_splits(bool bf16, int64_t na, int64_t nb, int64_t K) {
 constexpr int64_t kMaxThreads = 0xffffffffll;     // of a launch
 constexpr int64_t kMaxTrainRows = (1 << 24) - 1;  // a workgroup of 256 each
 
+constexpr int64_t kMaxTensors = int64_t(1) << 20;  // of a norm or clipping call
 constexpr int kNormSet = 180;      // tensors of one launch of the gradient norm
 constexpr int kNormBlocks = 1024;  // its workgroups, and partial sums, at most
 inline int64_t norm_parts(int64_t n) { return (n + kNormSet - 1) / kNormSet * kNormBlocks; }

@@ -52,3 +52,14 @@ def test_loss_workspace_part_by_part(rows):
     d, V = 4096, 151936
     parts = [4, 4 * rows, 16 * rows, 4 * rows * d, 4 * rows * (V // 32), 4 * rows]
     assert D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL, rows, 1, 1, d, V) == sum(_up(n, 256) for n in parts)
+
+
+def test_norm_workspace_is_sized_for_what_the_call_takes():
+    """dbl_grad_norm takes up to 2^20 tensors: more have no workspace (the product of a count near 2^62 and
+    the partial sums of a launch does not fit 64 bits either)."""
+    size = lambda n: D.dbl_workspace_bytes(D.DBL_OP_GRAD_NORM, n, 1, 1, 1, 1)
+    assert size(0) == 0
+    assert size(1) == size(180) == 1024 * 8 and size(181) == 2 * 1024 * 8
+    assert size(1 << 20) == -(-(1 << 20) // 180) * 1024 * 8
+    for n in ((1 << 20) + 1, 1 << 40, 3 * 10 ** 18, (1 << 61) + 12345):
+        assert size(n) == SIZE_MAX, n
