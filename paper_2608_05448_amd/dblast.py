@@ -153,9 +153,15 @@ def _workspace(op, shape, device, ws=None):
     n = _workspace_bytes(op, shape.B, shape.K, shape.R, shape.d, shape.V)
     if n == 0:
         return None, 0
-    if ws is not None:
+    if ws is not None:  # any type; one piece of GPU memory, as the kernels write it
+        if not isinstance(ws, torch.Tensor):
+            raise TypeError("the workspace must be a torch.Tensor")
+        if not ws.is_contiguous():
+            raise ValueError("the workspace must be contiguous")
         if ws.numel() * ws.element_size() < n:
             raise ValueError(f"workspace needs {n} bytes")
+        if not ws.is_cuda:
+            raise ValueError("the workspace must be a GPU tensor")
         return ws, ws.numel() * ws.element_size()
     return torch.empty(n, dtype=torch.uint8, device=device), n
 

@@ -63,3 +63,21 @@ def test_norm_workspace_is_sized_for_what_the_call_takes():
     assert size(1 << 20) == -(-(1 << 20) // 180) * 1024 * 8
     for n in ((1 << 20) + 1, 1 << 40, 3 * 10 ** 18, (1 << 61) + 12345):
         assert size(n) == SIZE_MAX, n
+
+
+def test_a_workspace_that_is_not_memory_in_one_piece_is_refused():
+    """The kernels write the whole size from the tensor's first byte on: a view that repeats or skips elements
+    has the number of elements, but not the memory."""
+    shape = D.Shape(1, 4, 2, 64, 256)
+    n = D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL, 1, 4, 2, 64, 256)
+    dev = torch.device("cuda", 0)
+    for ws in (torch.empty(1, dtype=torch.uint8).expand(n), torch.empty(2 * n, dtype=torch.uint8)[::2],
+               torch.empty((64, n), dtype=torch.uint8).t()):
+        with pytest.raises(ValueError, match="contiguous"):
+            D._workspace(D.DBL_OP_HEAD_NLL, shape, dev, ws)
+    with pytest.raises(ValueError, match="GPU tensor"):
+        D._workspace(D.DBL_OP_HEAD_NLL, shape, dev, torch.empty(n, dtype=torch.uint8))
+    with pytest.raises(ValueError, match=f"needs {n} bytes"):
+        D._workspace(D.DBL_OP_HEAD_NLL, shape, dev, torch.empty(n - 1, dtype=torch.uint8))
+    with pytest.raises(TypeError, match="torch.Tensor"):
+        D._workspace(D.DBL_OP_HEAD_NLL, shape, dev, bytearray(n))
