@@ -147,11 +147,12 @@ def dbl_workspace_bytes(op: int, B: int, K: int, R: int, d: int, V: int) -> int:
 
 # Looked up by a shape's own fields, which are plain integers, never by a caller's objects.
 _workspace_bytes = functools.lru_cache(maxsize=1024)(dbl_workspace_bytes)
+_NO_SIZE = ctypes.c_size_t(-1).value  # of a shape that is refused
 
 
 def _workspace(op, shape, device, ws=None):
     n = _workspace_bytes(op, shape.B, shape.K, shape.R, shape.d, shape.V)
-    if n == 0:
+    if n == 0 or n == _NO_SIZE:  # none needed; a shape that the call itself refuses, saying why
         return None, 0
     if ws is not None:  # any type; one piece of GPU memory, as the kernels write it
         if not isinstance(ws, torch.Tensor):

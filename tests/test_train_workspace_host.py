@@ -81,3 +81,20 @@ def test_a_workspace_that_is_not_memory_in_one_piece_is_refused():
         D._workspace(D.DBL_OP_HEAD_NLL, shape, dev, torch.empty(n - 1, dtype=torch.uint8))
     with pytest.raises(TypeError, match="torch.Tensor"):
         D._workspace(D.DBL_OP_HEAD_NLL, shape, dev, bytearray(n))
+
+
+def test_a_shape_without_a_workspace_is_left_to_the_call_to_refuse():
+    """No memory is asked for: the call's own check of the shape comes before that of the workspace, and says
+    what is wrong."""
+    shape = D.Shape(1, 1, 65, 8, 16)  # R <= 64
+    assert D.dbl_workspace_bytes(D.DBL_OP_HEAD_NLL, 1, 1, 65, 8, 16) == SIZE_MAX
+    assert D._workspace(D.DBL_OP_HEAD_NLL, shape, torch.device("cpu")) == (None, 0)
+    lib = D.load()
+    at = [ctypes.c_void_p(0x1000 * (i + 1)) for i in range(8)]
+    none = ctypes.c_void_p(None)
+    assert lib.dbl_head_nll(shape, D.DBL_BF16, *at[:5], none, 0, none) == D.DBL_ESHAPE
+    assert lib.dbl_head_nll_backward(shape, D.DBL_BF16, *at[:8], none, 0, none) == D.DBL_ESHAPE
+    many = D.Shape(1 << 24, 1, 1, 8, 16)
+    assert D._workspace(D.DBL_OP_HEAD_NLL, many, torch.device("cpu")) == (None, 0)
+    assert lib.dbl_head_nll(many, D.DBL_BF16, *at[:5], none, 0, none) == D.DBL_ESHAPE
+    assert D._workspace(D.DBL_OP_EXPAND_BACKWARD, many, torch.device("cpu")) == (None, 0)
