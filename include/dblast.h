@@ -428,7 +428,8 @@ dbl_status dbl_head_nll(dbl_shape shape, int dt, const void* h, const void* w, c
  * the logits formed again, a piece of the vocabulary at a time, and never kept whole. Positions that do
  * not count (x outside [0, V)) get dh = 0 and add nothing to dw, whatever their h and g hold.
  * fp32 accumulation; with bf16, u over (1 - p[x]) and h times g (1 - p[x]) are rounded to bf16 between
- * the two matrix products, and the results once at the end.
+ * the two matrix products, and the results once at the end. In a row that is sure of its token to within the
+ * rounding of nll, the gradient is off by about g times that rounding.
  *   nll, lse   as dbl_head_nll gave them for the same h, w and x
  *   g     [B, K, R] fp32
  *   dh    out [B, K, R, d] of type dt;  dw  out [V, d] of type dt, or NULL (the head is frozen)
@@ -448,14 +449,16 @@ dbl_status dbl_head_nll_backward(dbl_shape shape, int dt, const void* h, const v
  * branch states (the dh of dbl_head_nll_backward):
  *     dh[b, k]   = sum_z (dout[b, k, z] + W_z^T dout[b, k, z]),
  *     dW[z*d + i, j] = sum_{b,k} dout[b, k, z, i] h[b, k, j],   dc[z*d + i] = sum_{b,k} dout[b, k, z, i]
- * with fp32 accumulation, each rounded once to bf16.
+ * with fp32 accumulation, each rounded once to bf16. Every position is a term of the sums: one whose dout is 0
+ * (padding, after dbl_head_nll_backward) adds 0 to dW as long as its h is finite.
  *   shape   B, K, R, d used (V unused); d % 32 == 0, R*d <= 2^23, B*K < 2^24
  *   h       [B, K, d] bf16 trunk states;  W  [R*d, d] bf16;  dout  [B, K, R, d] bf16
  *   dh      out [B, K, d] bf16 or NULL;  dW  out [R*d, d] bf16 or NULL;  dc  out [R*d] bf16 or NULL
  *   ws      workspace of dbl_workspace_bytes(DBL_OP_EXPAND_BACKWARD, shape) bytes (V = 1), needed for dh and dW;
  *           otherwise may be 0 and NULL
  * The outputs may overlap neither each other nor an input. B = 0 sets dW and dc to 0.
- * Errors: DBL_EINVAL for null inputs, misaligned pointers or no output; DBL_ESHAPE; DBL_EWORKSPACE.
+ * Errors: DBL_EINVAL for null inputs, misaligned or overlapping pointers or no output; DBL_ESHAPE;
+ * DBL_EWORKSPACE; DBL_EHIP.
  */
 dbl_status dbl_expand_branches_backward(dbl_shape shape, const void* h, const void* W,
                                         const void* dout, void* dh, void* dW, void* dc, void* ws,

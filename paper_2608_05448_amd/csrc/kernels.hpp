@@ -146,10 +146,13 @@ struct DeterminismArgs {
 // One row that is trained on, as the head's training kernels see it. The gradient of its negative
 // log-likelihood with respect to the logits, g (p_v - [v = token]), is handled as scale * u_v with
 // u_v = exp(logit_v - shift') (shift' = lse + ln q) and u = at_token at the token.
-// bf16: q = 1 - p_token = -expm1(-nll), scale = g q, so that u is -1 at the token (exact in bf16) and in
-// [0, 1] elsewhere: the rounding of u to bf16 then touches the other ids only, whose errors average out,
-// and never the one entry that most of the gradient rests on. q is kept from below by 2^-24, the rounding
-// of a binary32 probability near 1 (at_token = -(1 - p) / q there). fp32: q = 1.
+// bf16: q = 1 - p_token = -expm1(-nll), scale = g q, so that u is -1 at the token (exact in bf16) and p_v / q
+// elsewhere: the rounding of u to bf16 then touches the other ids only, whose errors average out, and never
+// the one entry that most of the gradient rests on. q is kept from below by 2^-24, the rounding of a binary32
+// probability near 1 (at_token = -(1 - p) / q there, in [-1, 0]). nll = lse - logit is off by lse's rounding
+// (about 2e-6 at 20), and q with it: in a row that is as sure of its token as that, the other ids' u may be
+// above 1 and do not add up to the token's, which leaves the gradient off by about g times nll's error, as it
+// is in binary32 throughout. fp32: q = 1.
 struct alignas(16) TrainRow {
   float shift;     // bf16: (lse + ln q) log2(e); fp32: lse
   float at_token;
@@ -239,7 +242,9 @@ inline int64_t nll_piece(int64_t M, int64_t V, int elem) {
 // sums with both operands across them, a stream over the output. The last against the smaller tiles, us
 // (terms x output columns x rows): 200 x 4096 x 151936 317 and 477, 128 x 4096 x 151936 213 and 246, 256 x
 // 4096 x 32768 72 and 96, 100 x 2048 x 50000 38 and 50; but 168 x 1000 x 50257 34 and 31, 250 x 1024 x
-// 20000 25 and 20, 60 x 2560 x 151936 125 and 128, 30 x 2048 x 151936 118 and 107.
+// 20000 25 and 20, 60 x 2560 x 151936 125 and 128, 30 x 2048 x 151936 118 and 107. The smaller tiles against
+// the 256 x 256 ones below 512 terms: 300 x 4096 x 151936 548 and 609, 400 x 2048 x 50000 118 and 127, 480 x
+// 2560 x 151936 453 and 460.
 enum ProdKind : int { kProdPp = 0, kProdFew = 1, kProdSmall = 2, kProdStream = 3 };
 inline ProdKind prod_kind(bool both, int64_t na, int64_t nb, int64_t K) {
   if (na > 128 && nb > 128 && K >= 512) return kProdPp;
@@ -289,8 +294,9 @@ inline int grad_splits_f32(int64_t na, int64_t nb, int64_t K) {
 // The same for a product with both operands across the sum (the weight gradients): small outputs of many
 // rows would leave most CUs idle. The split with the least time, in ns: whole rounds of 256 workgroups, a
 // stage's time in each and 5 us for its ends; parts written and read at 5 TB/s, and one more launch. One part,
-// and that split, us: 1000 x 512 outputs of 8192 rows 145 and 30; 2048 x 512 of 4096 rows 75 and 29; fp32
-// 2000 x 256 of 8192 rows 380 and 116, 256 x 64 of 2048 rows 97 and 15.
+// and that split with the launch that adds the parts, us: 1000 x 512 outputs of 8192 rows 145 and 30 (24 + 6);
+// 2048 x 512 of 4096 rows 75 and 29 (22 + 7); fp32 2000 x 256 of 8192 rows 380 and 114 (109 + 5), 256 x 64 of
+// 2048 rows 97 and 14 (11 + 3).
 inline int weight_splits(bool bf16, int64_t na, int64_t nb, int64_t K) {
   if (na <= 0 || nb <= 0 || K <= 0) return 1;
   const ProdKind kind = bf16 ? prod_kind(true, na, nb, K) : kProdSmall;

@@ -4,6 +4,10 @@ Argument marshalling only: tensors are checked for device, dtype, layout and sha
 device pointers and the current HIP stream are passed to the library, and a workspace tensor
 is allocated when the call needs one. Every step of the computation runs in the library's
 kernels. There is no fallback: if the library is not built or no GPU is visible, calls raise.
+
+The calls take no part in autograd: results require no gradient even where arguments do (the training
+operators are the gradients, called one after the other), and what a call writes into a tensor it is given
+does not count as an in-place change of it.
 """
 from __future__ import annotations
 

@@ -137,15 +137,15 @@ HEAD_CASES = [
     ("bf16", 1, 1, 4, 128, 1000, "none"),       # few rows, 64-row tiles
     ("bf16", 2, 15, 4, 192, 2000, "some"),      # 120 rows, 128-row tiles
     ("bf16", 1, 15, 4, 64, 50001, "first"),     # 60 rows, tiles of 256 ids
-    ("bf16", 2, 16, 8, 128, 1500, "some"),      # 256 rows: 256 x 256 tiles
+    ("bf16", 2, 16, 8, 128, 1500, "some"),      # 256 rows, too few ids for the larger tiles: 128 x 128
     ("bf16", 3, 11, 9, 64, 1031, "some"),       # 297 rows, ragged in every direction
-    ("bf16", 2, 5, 3, 96, 700, "some"),         # d % 32: the four-wave copy kernel
-    ("bf16", 2, 5, 3, 200, 700, "but-last"),    # d % 8: the register-staged kernel
+    ("bf16", 2, 5, 3, 96, 700, "some"),         # d % 64 = 32: half a last stage
+    ("bf16", 2, 5, 3, 200, 700, "but-last"),    # d % 64 = 8: one chunk of a last stage
     ("bf16", 5, 13, 5, 72, 1153, "some"),
     ("bf16", 2, 4, 2, 64, 300, "all"),
     ("bf16", 1, 70, 1, 2048, 9000, "some"),     # sums that start further on
-    ("bf16", 1, 33, 1, 104, 513, "some"),       # a partial last stage: 64-row tiles, 128-row tiles,
-    ("bf16", 2, 40, 1, 1000, 901, "some"),      # 256-row tiles, and a hidden size below one stage
+    ("bf16", 1, 33, 1, 104, 513, "some"),       # a partial last stage: 64-row tiles, 128-row tiles, two
+    ("bf16", 2, 40, 1, 1000, 901, "some"),      # of them, and a hidden size below one stage
     ("bf16", 6, 40, 1, 136, 901, "some"),
     ("bf16", 2, 70, 2, 8, 2100, "some"),
     ("bf16", 3, 100, 1, 192, 600, "some"),      # 300 rows: the products' 256 x 256 tiles, short sums
