@@ -22,6 +22,10 @@
  *   dbl_head_nll / dbl_head_nll_backward  the loss of given tokens under the head and its gradient
  *   dbl_expand_branches_backward  gradients of the expander's weight, bias and trunk states
  *   dbl_grad_norm / dbl_clip_grads  the global norm of a set of gradients, and clipping to it
+ *   dbl_mx_quantize / dbl_mx_dequantize / dbl_add_rmsnorm_mx  rows in microscaled 4 or 8 bits
+ *   dbl_mx_matmul / dbl_mx_head_logprobs  logits, or branch log-probabilities, of such rows against a
+ *                       head in 4 bits
+ *   dbl_sample_logits   one token per row of logits under temperature, top-k, top-p and min-p
  *   dbl_target_logprobs / dbl_early_determinism  the target side: the sampling transform that
  *                       defines p, and the target-block early-determinism estimate
  *
@@ -112,7 +116,9 @@ typedef enum {
   DBL_OP_HEAD_NLL = 16,
   DBL_OP_HEAD_NLL_BACKWARD = 17,
   DBL_OP_EXPAND_BACKWARD = 18,
-  DBL_OP_GRAD_NORM = 19          /* dbl_grad_norm: shape.B tensors (K = R = d = V = 1) */
+  DBL_OP_GRAD_NORM = 19,         /* dbl_grad_norm: shape.B tensors (K = R = d = V = 1) */
+  DBL_OP_MX_HEAD = 32,           /* dbl_mx_head_logprobs: as DBL_OP_HEAD */
+  DBL_OP_SAMPLE_LOGITS = 33      /* dbl_sample_logits: rows N = shape.B * shape.K, shape.V */
 } dbl_op;
 
 typedef struct {
@@ -497,6 +503,115 @@ dbl_status dbl_grad_norm(int64_t n, const void* const* grads, const int64_t* num
 dbl_status dbl_clip_grads(int64_t n, const void* const* grads, void* const* out,
                           const int64_t* numel, const int32_t* dt, const float* norm,
                           float max_norm, void* stream);
+
+/*
+ * Microscaled rows. A row of d values is padded with zeros to dp = dbl_mx_row(d) = 128 ceil(d / 128) and
+ * held as dp codes and dp / 32 scales, a scale for each block of 32 consecutive values (the block format
+ * of the OCP Microscaling Formats specification):
+ *   bits 4   codes e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), two to a byte, the even value
+ *            in the low half: codes [M, dp / 2]
+ *   bits 8   codes e4m3 (up to 448): codes [M, dp]
+ *   scales   [M, dp / 32], a byte b for 2^(b - 127); 255 is NaN
+ * Rounding: with E = 2 (4 bits) or 8, a block's scale is 2^(floor(log2 max|x|) - E), at least 2^-127, and
+ * a value over it is rounded to the nearest code, ties to the even code, and to the largest one where it
+ * is beyond it. A block that holds an infinity or NaN has scale 255 and codes 0: all its values are NaN.
+ */
+int64_t dbl_mx_row(int64_t d);
+
+/*
+ * dbl_mx_quantize - rows x [M, d] of type dt in microscaled form.
+ *   M >= 0, 1 <= d <= 2^20;  dt DBL_BF16 or DBL_F32;  bits 4 or 8
+ *   codes, scales   out, as above, padding included
+ * dbl_mx_dequantize - the values of microscaled rows as type dt, rounded once: out [M, d]. (What
+ * dbl_mx_quantize gave is exact in either type, as long as it is in the type's range.)
+ * The outputs may overlap neither each other nor an input. Errors: DBL_EINVAL for null, misaligned or
+ * overlapping pointers or other bits; DBL_EDTYPE; DBL_ESHAPE.
+ */
+dbl_status dbl_mx_quantize(int64_t M, int64_t d, int dt, const void* x, int bits, void* codes,
+                           uint8_t* scales, void* stream);
+dbl_status dbl_mx_dequantize(int64_t M, int64_t d, int bits, const void* codes, const uint8_t* scales,
+                             int dt, void* out, void* stream);
+
+/*
+ * dbl_add_rmsnorm_mx - the norm in front of the head (or of the next projection), quantised:
+ *     sum = x + residual,   y = sum / sqrt(mean_j sum_j^2 + eps) * weight,
+ * the addition in fp32 and rounded once to dt, and the norm taken of that rounded sum (what later layers
+ * see); y stays in fp32 until it is quantised.
+ *   x, residual   [M, d] of type dt; residual may be NULL (then sum is x, and is not written)
+ *   weight        [d] of type dt;  eps >= 0, finite
+ *   sum           out [M, d] of type dt, NULL if it is not wanted or there is no residual; may be x or
+ *                 residual itself (in place)
+ *   bits, codes, scales   y in microscaled form, as dbl_mx_quantize
+ *   y             out [M, d] of type dt or NULL: y itself, rounded once
+ * Otherwise the outputs may overlap neither each other nor an input. A row of zeros with eps = 0 gives NaN.
+ * Errors: as dbl_mx_quantize, and DBL_EINVAL for eps < 0 or not finite, or sum without residual.
+ */
+dbl_status dbl_add_rmsnorm_mx(int64_t M, int64_t d, int dt, const void* x, const void* residual,
+                              const void* weight, float eps, void* sum, int bits, void* codes,
+                              uint8_t* scales, void* y, void* stream);
+
+/*
+ * dbl_mx_matmul - logits of microscaled states against a head in microscaled 4 bits,
+ *     logits[m, v] = sum_j h[m, j] w[v, j],  m < M, v < V,
+ * over the values that the codes stand for, summed in fp32 and rounded once to the type of the logits.
+ * With fp32 logits no product is cut; with bf16 logits and 8-bit states, products are cut at 2^-13 of the
+ * largest in their group of eight (below the rounding of the result). A row's logits do not depend on the
+ * other rows.
+ *   bits   of h, 4 or 8;  h, hs   [M, dp] states;  w, ws   [V, dp] 4-bit head
+ *   dt     DBL_F32 or DBL_BF16: type of logits, out [M, V]
+ * No workspace. M >= 0, 1 <= V < 2^24, 1 <= d <= 2^20. Errors: DBL_EINVAL, DBL_EDTYPE, DBL_ESHAPE, DBL_EHIP (where a
+ * launch would need 2^32 threads).
+ *
+ * dbl_mx_head_logprobs - dbl_head_logprobs for microscaled operands: the same outputs (the two-level form
+ * that dbl_sample_block, dbl_verify_block and the others read) of the same logits as dbl_mx_matmul's in
+ * fp32.
+ *   shape   B, K, R, d, V;  h, hs  M = B*K*R rows;  w, ws  [V, dp]
+ *   ws_mem  workspace of dbl_workspace_bytes(DBL_OP_MX_HEAD, shape) bytes, needed only with argmax
+ * The outputs of both may overlap neither each other nor an input. Errors: as dbl_head_logprobs, and DBL_EINVAL
+ * for bits.
+ */
+dbl_status dbl_mx_matmul(int64_t M, int64_t V, int64_t d, int bits, const void* h, const uint8_t* hs,
+                         const void* w, const uint8_t* ws, int dt, void* logits, void* stream);
+dbl_status dbl_mx_head_logprobs(dbl_shape shape, int bits, const void* h, const uint8_t* hs, const void* w,
+                                const uint8_t* ws, float* tls, float* lmass, float* lse, int32_t* argmax,
+                                void* ws_mem, size_t ws_bytes, void* stream);
+
+/*
+ * dbl_sample_logits - one token per row of logits, under each row's own parameters, from given random
+ * words: the draw that dbl_target_logprobs' distribution describes, without writing the distribution.
+ * Per row, with s = fl32(logit / T), m = max s and integer weights W = floor(detexp32(fl32(s - m)) 2^40):
+ * top-k and then top-p keep what dbl_target_logprobs keeps (ties with the k-th value are kept; a nucleus
+ * is filled by decreasing s and increasing id); min-p then keeps the ids with W >= min_p 2^40, that
+ * is those at least min_p times as probable as the likeliest. The token is the smallest id whose
+ * inclusive cumulative W over the kept ids exceeds floor(word * sum(W) / 2^32). T = 0 takes the lowest-index
+ * maximum. A row's token does not depend on the other rows. Logits of minus infinity are never drawn.
+ *   N, V      rows and vocabulary, 1 <= V < 2^24;  dt DBL_F32 or DBL_BF16;  logits [N, V]
+ *   words     [N] uniform 32-bit words
+ *   params    temperature >= 0, finite; top_k >= 0 (0, or V and more: off); top_p in (0, 1] (1: off);
+ *             min_p in [0, 1] (0: off). Each an array [N] on the device or, where that is NULL, the
+ *             number beside it for every row
+ *   token     out [N] int32;  logprob  out [N] fp32: log of the probability with which it was drawn
+ * A row without a distribution (parameters of its arrays out of range, a NaN among its logits, its
+ * largest s infinite) gets token -1 and logprob NaN.
+ *   ws        workspace of dbl_workspace_bytes(DBL_OP_SAMPLE_LOGITS, shape) bytes, shape.B * shape.K = N
+ * token and logprob may overlap neither each other nor an input. Errors: DBL_EINVAL for null, misaligned or overlapping pointers
+ * (arrays of a value per row need their elements' alignment only) or numbers out of range; DBL_EDTYPE;
+ * DBL_ESHAPE; DBL_EWORKSPACE; DBL_EHIP (where a launch would need 2^32 threads).
+ */
+typedef struct {
+  float temperature;
+  float top_p;
+  float min_p;
+  int64_t top_k;
+  const float* temperatures;
+  const float* top_ps;
+  const float* min_ps;
+  const int32_t* top_ks;
+} dbl_sampling;
+
+dbl_status dbl_sample_logits(int64_t N, int64_t V, int dt, const void* logits, const uint32_t* words,
+                             dbl_sampling params, int32_t* token, float* logprob, void* ws,
+                             size_t ws_bytes, void* stream);
 
 /*
  * dbl_stream_read_probe - a diagnostic, not an operation of the method: reads every 16-byte

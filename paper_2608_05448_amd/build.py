@@ -2,8 +2,8 @@
 
     python -m paper_2608_05448_amd.build          # or: from paper_2608_05448_amd import build
 
-Every translation unit is compiled with packed-fp32 instructions disabled; the sampler and
-verifier units (every discrete decision of the determinism contract) are also compiled with
+Every translation unit is compiled with packed-fp32 instructions disabled; the sampler, verifier and
+token-draw units (every discrete decision of the determinism contract) are also compiled with
 floating-point contraction off.
 """
 from __future__ import annotations
@@ -32,6 +32,10 @@ SOURCES = {
     "abi_train.hip": [],
     "train.hip": [],
     "clip.hip": [],
+    "abi_serve.hip": [],
+    "quant.hip": [],
+    "mxhead.hip": [],
+    "draw.hip": ["-ffp-contract=off"],
 }
 COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-Wall",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

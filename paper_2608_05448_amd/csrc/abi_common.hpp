@@ -4,9 +4,11 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <initializer_list>
 #include <string>
 #include <utility>
+#include <vector>
 
 #include "../../include/dblast.h"
 #include "kernels.hpp"
@@ -66,6 +68,7 @@ inline WsLayout layout(int op, const dbl_shape& s) {
   int n = 0;
   switch (op) {
     case DBL_OP_HEAD:  // argmax keys, used only when argmax is requested
+    case DBL_OP_MX_HEAD:
       sizes[0] = B * K * R * sizeof(uint64_t);
       n = 1;
       break;
@@ -153,6 +156,16 @@ inline WsLayout layout(int op, const dbl_shape& s) {
       sizes[0] = static_cast<size_t>(dbl::norm_parts(s.B)) * sizeof(double);
       n = 1;
       break;
+    case DBL_OP_SAMPLE_LOGITS: {  // rows B*K
+      const size_t row = dbl::draw_row_bytes(s.V);
+      if (B * K > SIZE_MAX / 2 / row) {
+        L.total = SIZE_MAX;
+        return L;
+      }
+      sizes[0] = B * K * row;
+      n = 1;
+      break;
+    }
     default:
       L.total = SIZE_MAX;
       return L;
@@ -181,6 +194,39 @@ inline dbl_status check_ws(int op, const dbl_shape& s, void* ws, size_t ws_bytes
 inline dbl_status hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return ok();
   return fail(DBL_EHIP, std::string(what) + ": " + hipGetErrorString(e));
+}
+
+// A piece of memory that a call reads or writes.
+struct Span {
+  uintptr_t at, end;
+  bool written;
+  Span(const void* p, size_t bytes, bool w)
+      : at(reinterpret_cast<uintptr_t>(p)), end(at + (p ? bytes : 0)), written(w) {}
+};
+
+// Whether a written piece overlaps another one (sorted by address, the pieces written so far reach as far
+// as `written`, all as far as `any`).
+inline bool overlapping(std::vector<Span>& s) {
+  std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
+  uintptr_t any = 0, written = 0;
+  for (const Span& x : s) {
+    if (x.at == x.end) continue;
+    if (x.at < (x.written ? any : written)) return true;
+    any = std::max(any, x.end);
+    if (x.written) written = std::max(written, x.end);
+  }
+  return false;
+}
+
+// No C++ exception (a host allocation that fails) crosses the C boundary.
+template <class F>
+dbl_status guarded(F f) noexcept {
+  try {
+    return f();
+  } catch (...) {
+    g_last_error.clear();
+    return DBL_EHIP;
+  }
 }
 
 }  // namespace dbl_abi

@@ -16,28 +16,6 @@ using namespace dbl_abi;
 
 namespace {
 
-// A piece of memory that a call reads or writes.
-struct Span {
-  uintptr_t at, end;
-  bool written;
-  Span(const void* p, size_t bytes, bool w)
-      : at(reinterpret_cast<uintptr_t>(p)), end(at + (p ? bytes : 0)), written(w) {}
-};
-
-// Whether a written piece overlaps another one (sorted by address, the pieces written so far reach as far
-// as `written`, all as far as `any`).
-bool overlapping(std::vector<Span>& s) {
-  std::sort(s.begin(), s.end(), [](const Span& a, const Span& b) { return a.at < b.at; });
-  uintptr_t any = 0, written = 0;
-  for (const Span& x : s) {
-    if (x.at == x.end) continue;
-    if (x.at < (x.written ? any : written)) return true;
-    any = std::max(any, x.end);
-    if (x.written) written = std::max(written, x.end);
-  }
-  return false;
-}
-
 dbl_status check_nll(const dbl_shape& s, int dt) {
   if (dbl_status st = check_shape(s, true)) return st;
   if (dt != DBL_BF16 && dt != DBL_F32) return fail(DBL_EDTYPE, "dt must be DBL_BF16 or DBL_F32");
@@ -91,17 +69,6 @@ dbl_status check_tensors(int64_t n, const void* const* grads, const int64_t* num
       return fail(DBL_EINVAL, "a tensor is not aligned to its elements");
   }
   return ok();
-}
-
-// No C++ exception (a host allocation that fails) crosses the C boundary.
-template <class F>
-dbl_status guarded(F f) noexcept {
-  try {
-    return f();
-  } catch (...) {
-    g_last_error.clear();
-    return DBL_EHIP;
-  }
 }
 
 }  // namespace

@@ -318,6 +318,92 @@ inline int weight_splits(bool bf16, int64_t na, int64_t nb, int64_t K) {
   return best;
 }
 
+// Microscaled rows: blocks of 32 values that share a power of two (one byte b for 2^(b - 127)), in 4 bits
+// (e2m1, two to a byte, the even value low) or 8 (e4m3); a row of d values is padded with zeros to mx_row(d).
+constexpr int kMxBlock = 32, kMxPad = 128;
+inline int64_t mx_row(int64_t d) { return (d + kMxPad - 1) / kMxPad * kMxPad; }
+
+struct MxQuantArgs {
+  int64_t M;
+  int d, bits;
+  bool bf16;
+  const void* x;        // [M, d]; dequantisation: out
+  void* codes;          // [M, mx_row(d) * bits / 8]
+  uint8_t* scales;      // [M, mx_row(d) / 32]
+};
+
+// Norm: h = x + residual (rounded to the type), y = h / sqrt(mean(h^2) + eps) * weight.
+struct MxNormArgs {
+  MxQuantArgs q;
+  const void* residual; // [M, d] or null
+  const void* weight;   // [d]
+  float eps;
+  void* sum;            // [M, d] or null
+  void* y;              // [M, d] or null
+};
+
+// Product of microscaled rows h [M, d] (4 or 8 bits) and w [V, d] (4 bits): logits, or the head's
+// two-level form.
+struct MxProductArgs {
+  int64_t M, V;
+  int dp;               // mx_row(d)
+  int bits;             // of h
+  const void* h;
+  const uint8_t* hs;
+  const void* w;
+  const uint8_t* ws;
+  void* logits;         // [M, V], or null: the two-level form
+  bool bf16;            // type of the logits
+  float* tls;           // [M, V]
+  float* lmass;         // [M, nT]
+  float* lse;           // [M]
+  int32_t* argmax;      // [M] or null
+  uint64_t* amax_keys;  // workspace [M]
+};
+
+// One token per row of logits.
+struct DrawArgs {
+  int64_t N, V;
+  bool bf16;
+  const void* logits;   // [N, V]
+  const uint32_t* words;
+  float temperature, top_p, min_p;
+  int64_t top_k;
+  const float *temperatures, *top_ps, *min_ps;  // [N] or null: the number beside each
+  const int32_t* top_ks;
+  int32_t* token;       // [N]
+  float* logprob;       // [N]
+  char* ws;
+};
+// The draw's rows are split into segments of this many ids; a workgroup each.
+constexpr int kDrawSeg = 8192;
+// Segments of a row: up to 7 ids more than V, where a row starts inside a 16-byte word.
+inline int64_t draw_segments(int64_t V) { return (V + 7 + kDrawSeg - 1) / kDrawSeg; }
+constexpr int kDrawBins = 512, kDrawList = 4096;
+struct DrawState {       // of a row
+  uint32_t tickets[2];   // workgroups that are through with its second and third launch
+  uint32_t count;        // entries of the list
+  uint32_t mode;         // what the third launch does (see draw.hip)
+  uint32_t cut_bin, by;  // where the cut falls, and what makes it
+  uint64_t need;
+  uint64_t unused[4];
+};
+static_assert(sizeof(DrawState) == 64, "the row's arrays follow it");
+// A row's workspace, for G segments: the state; by segment the maximum and the sum; the list; by segment
+// the bins' masses and counts.
+struct DrawLayout {
+  size_t top, sum, list, mass, count, total;
+  __host__ __device__ explicit DrawLayout(int64_t G) {
+    top = sizeof(DrawState);
+    sum = top + 8 * G;
+    list = sum + 8 * G;
+    mass = list + 8 * kDrawList;
+    count = mass + 8 * static_cast<size_t>(kDrawBins) * G;
+    total = (count + 4 * static_cast<size_t>(kDrawBins) * G + 255) / 256 * 256;
+  }
+};
+inline size_t draw_row_bytes(int64_t V) { return DrawLayout(draw_segments(V)).total; }
+
 constexpr int64_t kMaxThreads = 0xffffffffll;     // of a launch
 constexpr int64_t kMaxTrainRows = (1 << 24) - 1;  // a workgroup of 256 each
 
@@ -347,6 +433,14 @@ hipError_t launch_clip_grads(const GradTensor* t, int64_t n, const float* norm, 
                              hipStream_t stream);
 hipError_t launch_filter(const FilterArgs& a, hipStream_t stream);
 hipError_t launch_determinism(const DeterminismArgs& a, hipStream_t stream);
+hipError_t launch_argmax_clear(uint64_t* amax, int64_t M, hipStream_t stream);
+hipError_t launch_lse(const float* lmass, float* lse, const uint64_t* amax, int32_t* argmax, int64_t M,
+                      int nT, hipStream_t stream);
+hipError_t launch_mx_quantize(const MxQuantArgs& a, hipStream_t stream);
+hipError_t launch_mx_dequantize(const MxQuantArgs& a, hipStream_t stream);
+hipError_t launch_mx_norm(const MxNormArgs& a, hipStream_t stream);
+hipError_t launch_mx_product(const MxProductArgs& a, hipStream_t stream);
+hipError_t launch_draw(const DrawArgs& a, hipStream_t stream);
 hipError_t launch_read_probe(const void* buf, int64_t bytes, float* partials, int64_t n_partials,
                              hipStream_t stream);
 

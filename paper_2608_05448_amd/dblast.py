@@ -27,12 +27,20 @@ DBL_F32, DBL_BF16 = 0, 1
 (DBL_OP_HEAD, DBL_OP_SAMPLE, DBL_OP_VERIFY, DBL_OP_EXPECTED_LEN, DBL_OP_SAMPLE_GREEDY,
  DBL_OP_VERIFY_GREEDY, DBL_OP_EXPECTED_LEN_GREEDY, DBL_OP_TARGET) = range(8)
 DBL_OP_HEAD_NLL, DBL_OP_HEAD_NLL_BACKWARD, DBL_OP_EXPAND_BACKWARD, DBL_OP_GRAD_NORM = range(16, 20)
+DBL_OP_MX_HEAD, DBL_OP_SAMPLE_LOGITS = 32, 33
 VTILE = 128
 
 
 class Shape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int64), ("K", ctypes.c_int64), ("R", ctypes.c_int64),
                 ("d", ctypes.c_int64), ("V", ctypes.c_int64)]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_p", ctypes.c_float),
+                ("min_p", ctypes.c_float), ("top_k", ctypes.c_int64),
+                ("temperatures", ctypes.c_void_p), ("top_ps", ctypes.c_void_p),
+                ("min_ps", ctypes.c_void_p), ("top_ks", ctypes.c_void_p)]
 
 
 class DblastError(RuntimeError):
@@ -79,6 +87,17 @@ _SIGS = {
     "dbl_clip_grads": (ctypes.c_int, [_I64, _P, _P, _P, _P, _P, _F, _P]),
     "dbl_target_logprobs": (ctypes.c_int, [_I64, _I64, _P, _F, _I64, _F, _P, _P, _SZ, _P]),
     "dbl_early_determinism": (ctypes.c_int, [_I64, _I64, _I64, _P, _P, _P, _P, _P]),
+    "dbl_mx_row": (_I64, [_I64]),
+    "dbl_mx_quantize": (ctypes.c_int, [_I64, _I64, ctypes.c_int, _P, ctypes.c_int, _P, _P, _P]),
+    "dbl_mx_dequantize": (ctypes.c_int, [_I64, _I64, ctypes.c_int, _P, _P, ctypes.c_int, _P, _P]),
+    "dbl_add_rmsnorm_mx": (ctypes.c_int, [_I64, _I64, ctypes.c_int, _P, _P, _P, _F, _P,
+                                          ctypes.c_int, _P, _P, _P, _P]),
+    "dbl_mx_matmul": (ctypes.c_int, [_I64, _I64, _I64, ctypes.c_int, _P, _P, _P, _P, ctypes.c_int,
+                                     _P, _P]),
+    "dbl_mx_head_logprobs": (ctypes.c_int, [Shape, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _P,
+                                            _SZ, _P]),
+    "dbl_sample_logits": (ctypes.c_int, [_I64, _I64, ctypes.c_int, _P, _P, Sampling, _P, _P, _P, _SZ,
+                                         _P]),
     "dbl_stream_read_probe": (ctypes.c_int, [_P, _I64, _P, _I64, _P]),
 }
 EXPORTED = tuple(_SIGS)
@@ -647,6 +666,193 @@ def dbl_early_determinism(x, logp):
     _check(load().dbl_early_determinism(M, b, logp.shape[-1], _ptr(x), _ptr(logp), _ptr(terms),
                                         _ptr(mean), _stream(dev)))
     return terms, mean
+
+
+_MX_SCALE = torch.float8_e8m0fnu
+_MX_CODES = {4: torch.uint8, 8: torch.float8_e4m3fn}
+_MX_BITS = {torch.uint8: 4, torch.float8_e4m3fn: 8}
+
+
+def mx_row(d: int) -> int:
+    """Values of a microscaled row of d: d up to the next multiple of 128."""
+    return (d + 127) // 128 * 128
+
+
+def _mx_out(rows, d, bits, device, codes, scales):
+    """Codes and scales of rows (a shape) of d values, new ones where they are not given."""
+    if bits not in _MX_CODES:
+        raise ValueError("bits must be 4 or 8")
+    dp = mx_row(d)
+    cs, ss = (*rows, dp * bits // 8), (*rows, dp // 32)
+    codes = torch.empty(cs, dtype=_MX_CODES[bits], device=device) if codes is None else codes
+    scales = torch.empty(ss, dtype=_MX_SCALE, device=device) if scales is None else scales
+    _need(codes, "codes", _MX_CODES[bits], cs)
+    _need(scales, "scales", _MX_SCALE, ss)
+    return codes, scales
+
+
+def _mx_in(codes, scales, name):
+    """Leading shape, values of a padded row and bits of microscaled rows."""
+    bits = _MX_BITS.get(codes.dtype)
+    if bits is None:
+        raise TypeError(f"{name} must be uint8 (4-bit codes) or float8_e4m3fn, got {codes.dtype}")
+    if codes.dim() < 1 or codes.shape[-1] == 0 or codes.shape[-1] % (16 * bits):
+        raise ValueError(f"{name} must be [..., {16 * bits} n], got {tuple(codes.shape)}")
+    _need(codes, name, codes.dtype)
+    dp = codes.shape[-1] * 8 // bits
+    _need(scales, f"{name}'s scales", _MX_SCALE, (*codes.shape[:-1], dp // 32))
+    return codes.shape[:-1], dp, bits
+
+
+def _rows(x, name):
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.dtype not in _GRAD_TYPES:
+        raise TypeError(f"{name} must be bfloat16 or float32")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"{name} must be [..., d]")
+    _need(x, name, x.dtype)
+    return x.shape[:-1], x.shape[-1], _GRAD_TYPES[x.dtype]
+
+
+def dbl_mx_quantize(x, bits=4, codes=None, scales=None):
+    """Rows x [..., d] (bf16 or fp32) in microscaled 4 or 8 bits: (codes, scales), with dp = mx_row(d).
+    codes: uint8 [..., dp / 2] (4 bits, the even value in the low half) or float8_e4m3fn [..., dp];
+    scales: float8_e8m0fnu [..., dp / 32]."""
+    rows, d, dt = _rows(x, "x")
+    dev = x.device
+    codes, scales = _mx_out(rows, d, bits, dev, codes, scales)
+    _same_device(dev, codes=codes, scales=scales)
+    _run(load().dbl_mx_quantize, dev, x.numel() // d, d, dt, _ptr(x), bits, _ptr(codes), _ptr(scales))
+    return codes, scales
+
+
+def dbl_mx_dequantize(codes, scales, d, dtype=torch.bfloat16, out=None):
+    """The values [..., d] (bf16 or fp32) that microscaled rows stand for."""
+    rows, dp, bits = _mx_in(codes, scales, "codes")
+    d = operator.index(d)
+    if d < 1 or mx_row(d) != dp:
+        raise ValueError(f"rows of {dp} values cannot hold d = {d}")
+    if dtype not in _GRAD_TYPES:
+        raise TypeError("dtype must be bfloat16 or float32")
+    dev = codes.device
+    out = torch.empty((*rows, d), dtype=dtype, device=dev) if out is None else out
+    _need(out, "out", dtype, (*rows, d))
+    _same_device(dev, scales=scales, out=out)
+    _run(load().dbl_mx_dequantize, dev, out.numel() // d, d, bits, _ptr(codes), _ptr(scales),
+         _GRAD_TYPES[dtype], _ptr(out))
+    return out
+
+
+def dbl_add_rmsnorm_mx(x, residual, weight, eps=1e-6, bits=8, want_y=False, sum=None, codes=None,
+                       scales=None, y=None):
+    """Norm of x + residual (x alone where ``residual`` is None), quantised: x and residual [..., d],
+    weight [d], all bf16 or all fp32 -> (sum [..., d], codes, scales), with ``want_y`` (or ``y``) also y
+    [..., d] before its quantisation. ``sum`` is None without a residual and may be x or residual (in place)."""
+    rows, d, dt = _rows(x, "x")
+    dev = x.device
+    if residual is not None:
+        _need(residual, "residual", x.dtype, x.shape)
+        sum = torch.empty_like(x) if sum is None else sum
+    elif sum is not None:
+        raise ValueError("sum needs a residual")
+    if sum is not None:
+        _need(sum, "sum", x.dtype, x.shape)
+    _need(weight, "weight", x.dtype, (d,))
+    codes, scales = _mx_out(rows, d, bits, dev, codes, scales)
+    if want_y or y is not None:
+        y = torch.empty_like(x) if y is None else y
+        _need(y, "y", x.dtype, x.shape)
+    _same_device(dev, residual=residual, weight=weight, sum=sum, codes=codes, scales=scales, y=y)
+    _run(load().dbl_add_rmsnorm_mx, dev, x.numel() // d, d, dt, _ptr(x), _ptr(residual), _ptr(weight),
+         float(eps), _ptr(sum), bits, _ptr(codes), _ptr(scales), _ptr(y))
+    return (sum, codes, scales) if y is None else (sum, codes, scales, y)
+
+
+def _mx_head(h, h_scales, w, w_scales):
+    rows, dp, bits = _mx_in(h, h_scales, "h")
+    wrows, wdp, wbits = _mx_in(w, w_scales, "w")
+    if wbits != 4 or len(wrows) != 1 or wdp != dp:
+        raise ValueError(f"w must be 4-bit codes [V, {dp // 2}]")
+    return rows, dp, bits, wrows[0]
+
+
+def dbl_mx_matmul(h, h_scales, w, w_scales, dtype=torch.float32, out=None):
+    """Logits [..., V] (fp32 or bf16) of microscaled states h [..., .] (4 or 8 bits) against a microscaled
+    4-bit head w [V, .] (``dbl_mx_quantize``)."""
+    rows, dp, bits, V = _mx_head(h, h_scales, w, w_scales)
+    if dtype not in _GRAD_TYPES:
+        raise TypeError("dtype must be bfloat16 or float32")
+    dev = h.device
+    out = torch.empty((*rows, V), dtype=dtype, device=dev) if out is None else out
+    _need(out, "out", dtype, (*rows, V))
+    _same_device(dev, h_scales=h_scales, w=w, w_scales=w_scales, out=out)
+    _run(load().dbl_mx_matmul, dev, rows.numel(), V, dp, bits, _ptr(h), _ptr(h_scales), _ptr(w),
+         _ptr(w_scales), _GRAD_TYPES[dtype], _ptr(out))
+    return out
+
+
+def dbl_mx_head_logprobs(h, h_scales, w, w_scales, tls=None, lmass=None, lse=None, argmax=None, ws=None):
+    """``dbl_head_logprobs`` for microscaled operands: h [B, K, R, .] (4 or 8 bits) and w [V, .] (4 bits),
+    as ``dbl_mx_quantize`` or ``dbl_add_rmsnorm_mx`` give them. The same outputs."""
+    rows, dp, bits, V = _mx_head(h, h_scales, w, w_scales)
+    if len(rows) != 3:
+        raise ValueError("h must be [B, K, R, .]")
+    B, K, R = rows
+    dev = h.device
+    tls = torch.empty((B, K, R, V), dtype=torch.float32, device=dev) if tls is None else tls
+    lmass = tls.new_empty((B, K, R, ntiles(V))) if lmass is None else lmass
+    lse = tls.new_empty((B, K, R)) if lse is None else lse
+    _need(tls, "tls", torch.float32, (B, K, R, V))
+    _need(lmass, "lmass", torch.float32, (B, K, R, ntiles(V)))
+    _need(lse, "lse", torch.float32, (B, K, R))
+    shape = Shape(B, K, R, dp, V)
+    want_arg = argmax is not None and argmax is not False
+    if want_arg:
+        if argmax is True:
+            argmax = torch.empty((B, K, R), dtype=torch.int32, device=dev)
+        _need(argmax, "argmax", torch.int32, (B, K, R))
+        ws, nws = _workspace(DBL_OP_MX_HEAD, shape, dev, ws)
+    else:
+        argmax, ws, nws = None, None, 0
+    _same_device(dev, h_scales=h_scales, w=w, w_scales=w_scales, tls=tls, lmass=lmass, lse=lse,
+                 argmax=argmax, ws=ws)
+    _run(load().dbl_mx_head_logprobs, dev, shape, bits, _ptr(h), _ptr(h_scales), _ptr(w),
+         _ptr(w_scales), _ptr(tls), _ptr(lmass), _ptr(lse), _ptr(argmax), _ptr(ws), nws)
+    return (tls, lmass, lse, argmax) if want_arg else (tls, lmass, lse)
+
+
+def dbl_sample_logits(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None,
+                      logprob=None, ws=None):
+    """One token per row of logits [..., V] (fp32 or bf16) from random words [...] (int32, all 32 bits
+    uniform: ``torch.randint(-2**31, 2**31, shape, dtype=torch.int32)``), under temperature, top-k, top-p and
+    min-p: numbers, or a tensor [...] with a value for every row (fp32; top_k int32). Returns (token
+    [...] int32, logprob [...] fp32), logprob of the probability with which the token was drawn."""
+    rows, V, dt = _rows(logits, "logits")
+    dev = logits.device
+    _need(words, "words", torch.int32, rows)
+    token = torch.empty(rows, dtype=torch.int32, device=dev) if token is None else token
+    logprob = torch.empty(rows, dtype=torch.float32, device=dev) if logprob is None else logprob
+    _need(token, "token", torch.int32, rows)
+    _need(logprob, "logprob", torch.float32, rows)
+    p = Sampling(1.0, 1.0, 0.0, 0, None, None, None, None)
+    given = {}
+    for name, many, value, dtype, plain in (("temperature", "temperatures", temperature, torch.float32, float),
+                                            ("top_k", "top_ks", top_k, torch.int32, operator.index),
+                                            ("top_p", "top_ps", top_p, torch.float32, float),
+                                            ("min_p", "min_ps", min_p, torch.float32, float)):
+        if isinstance(value, torch.Tensor):
+            _need(value, name, dtype, rows)
+            given[name] = value
+            setattr(p, many, _ptr(value))
+        else:
+            setattr(p, name, plain(value))
+    N = logits.numel() // V
+    ws, nws = _workspace(DBL_OP_SAMPLE_LOGITS, Shape(N, 1, 1, 0, V), dev, ws)
+    _same_device(dev, words=words, token=token, logprob=logprob, ws=ws, **given)
+    _run(load().dbl_sample_logits, dev, N, V, dt, _ptr(logits), _ptr(words), p, _ptr(token),
+         _ptr(logprob), _ptr(ws), nws)
+    return token, logprob
 
 
 def dbl_stream_read_probe(buf, partials):
