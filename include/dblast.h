@@ -536,7 +536,7 @@ dbl_status dbl_mx_dequantize(int64_t M, int64_t d, int bits, const void* codes, 
  * dbl_add_rmsnorm_mx - the norm in front of the head (or of the next projection), quantised:
  *     sum = x + residual,   y = sum / sqrt(mean_j sum_j^2 + eps) * weight,
  * the addition in fp32 and rounded once to dt, and the norm taken of that rounded sum (what later layers
- * see); y stays in fp32 until it is quantised.
+ * see), in binary64; y is rounded once, to its codes.
  *   x, residual   [M, d] of type dt; residual may be NULL (then sum is x, and is not written)
  *   weight        [d] of type dt;  eps >= 0, finite
  *   sum           out [M, d] of type dt, NULL if it is not wanted or there is no residual; may be x or

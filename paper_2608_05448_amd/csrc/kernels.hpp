@@ -376,30 +376,31 @@ struct DrawArgs {
   char* ws;
 };
 // The draw's rows are split into segments of this many ids; a workgroup each.
-constexpr int kDrawSeg = 8192;
+constexpr int kDrawSeg = 4096;
 // Segments of a row: up to 7 ids more than V, where a row starts inside a 16-byte word.
 inline int64_t draw_segments(int64_t V) { return (V + 7 + kDrawSeg - 1) / kDrawSeg; }
-constexpr int kDrawBins = 512, kDrawList = 4096;
+constexpr int kDrawBins = 4096, kDrawList = 4096;
 struct DrawState {       // of a row
-  uint32_t tickets[2];   // workgroups that are through with its second and third launch
   uint32_t count;        // entries of the list
-  uint32_t mode;         // what the third launch does (see draw.hip)
+  uint32_t mode;         // what the launches that follow do (see draw.hip)
   uint32_t cut_bin, by;  // where the cut falls, and what makes it
   uint64_t need;
-  uint64_t unused[4];
+  float low;             // logits below it are not kept
+  uint32_t unused[9];
 };
 static_assert(sizeof(DrawState) == 64, "the row's arrays follow it");
-// A row's workspace, for G segments: the state; by segment the maximum and the sum; the list; by segment
-// the bins' masses and counts.
+// A row's workspace, for G segments: the state; by segment the maximum, the sum and the maxima of 128 ids
+// each; the list; the bins' masses and counts.
 struct DrawLayout {
-  size_t top, sum, list, mass, count, total;
+  size_t top, sum, maxima, list, mass, count, total;
   __host__ __device__ explicit DrawLayout(int64_t G) {
     top = sizeof(DrawState);
     sum = top + 8 * G;
-    list = sum + 8 * G;
+    maxima = sum + 8 * G;
+    list = (maxima + kDrawSeg / 128 * 4 * G + 255) / 256 * 256;
     mass = list + 8 * kDrawList;
-    count = mass + 8 * static_cast<size_t>(kDrawBins) * G;
-    total = (count + 4 * static_cast<size_t>(kDrawBins) * G + 255) / 256 * 256;
+    count = mass + 8 * kDrawBins;
+    total = count + 4 * kDrawBins;
   }
 };
 inline size_t draw_row_bytes(int64_t V) { return DrawLayout(draw_segments(V)).total; }

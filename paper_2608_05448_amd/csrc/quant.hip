@@ -191,22 +191,33 @@ __device__ __forceinline__ float as(float x) {
   return static_cast<float>(static_cast<T>(x));
 }
 
-__device__ __forceinline__ float wave_sum(float v) {
+__device__ __forceinline__ double wave_sum(double v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
 
+// binary64 to binary32 so that a further rounding to fewer bits gives what rounding the binary64 number
+// would: towards zero, and odd where bits are lost. (Infinite only where x is.)
+__device__ __forceinline__ float round_odd(double x) {
+  const float f = static_cast<float>(x);
+  const double b = static_cast<double>(f);
+  const uint32_t u = __float_as_uint(f);
+  return __uint_as_float(b == x ? u : ((fabs(b) > fabs(x) ? u - 1 : u) | 1u));
+}
+
 // Norm with the residual's addition. TPR threads take a row (256 / TPR rows to a workgroup), ITEMS
 // groups of eight values each, which stay in registers between the sum of squares and the result, so that
-// every input is read once. ITEMS = 0: rows of any length, read a second time (h from `sum`, which the
+// every input is read once. The sum, the root and the products are in binary64 and y is rounded once, to
+// its code: they hide behind the memory (16,384 rows of 4,096: 85 us in binary32), and a value near a
+// border between two codes falls on its own side of it. ITEMS = 0: rows of any length, read a second time (h from `sum`, which the
 // same thread has written, if there is one).
 template <class T, int BITS, bool VEC, int TPR, int ITEMS>
 __global__ __launch_bounds__(256) void norm_kernel(const T* x, const T* residual, const T* __restrict__ weight,
                                                    float eps, T* sum, T* y, uint8_t* __restrict__ codes,
                                                    uint8_t* __restrict__ scales, int64_t M, int d, int dp) {
   constexpr int ROWS = 256 / TPR;
-  __shared__ float part[4];
+  __shared__ double part[4];
   const int64_t row = static_cast<int64_t>(blockIdx.x) * ROWS + threadIdx.x / TPR;
   const int t = threadIdx.x % TPR;
   if (TPR == 64 && row >= M) return;  // whole wavefronts; TPR == 256: a workgroup per row
@@ -215,7 +226,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T* x, const T* residual
   T* const sr = sum ? sum + row * d : nullptr;
   constexpr int kHeld = ITEMS ? ITEMS : 1;
   float h[kHeld][8];
-  float ss = 0.0f;
+  double ss = 0.0;
   auto take = [&](int j, float (&v)[8]) {
     load8<T, VEC>(xr, j, d, v);
     if (rr) {
@@ -226,7 +237,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T* x, const T* residual
       if (sr) store8<T, VEC>(sr, j, d, v);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(v[i], v[i], ss);
+    for (int i = 0; i < 8; ++i) ss = fma(static_cast<double>(v[i]), static_cast<double>(v[i]), ss);
   };
   if constexpr (ITEMS > 0) {
 #pragma unroll
@@ -243,13 +254,17 @@ __global__ __launch_bounds__(256) void norm_kernel(const T* x, const T* residual
     __syncthreads();
     ss = (part[0] + part[1]) + (part[2] + part[3]);
   }
-  const float scale = 1.0f / sqrtf(ss / static_cast<float>(d) + eps);
+  const double scale = 1.0 / sqrt(ss / static_cast<double>(d) + static_cast<double>(eps));
   auto give = [&](int j, float (&v)[8]) {
     float w[8];
     load8<T, VEC>(weight, j, d, w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = v[i] * scale * w[i];
-    if (y) store8<T, VEC>(y + row * d, j, d, v);
+    for (int i = 0; i < 8; ++i) {
+      const double p = static_cast<double>(v[i]) * scale * static_cast<double>(w[i]);
+      v[i] = round_odd(p);
+      w[i] = sizeof(T) == 4 ? static_cast<float>(p) : v[i];
+    }
+    if (y) store8<T, VEC>(y + row * d, j, d, w);
     quantize8<BITS>(v, codes + row * (dp / 8 * BITS), scales + row * (dp / 32), j);
   };
   if constexpr (ITEMS > 0) {

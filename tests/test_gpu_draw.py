@@ -11,7 +11,7 @@ from oracle import contract as C
 
 pytestmark = pytest.mark.gpu
 
-SEG = 8192  # ids of a row that one workgroup takes
+SEG = 4096  # ids of a row that one workgroup takes at a time
 
 
 def plain(x, T, k, p, least, word):
@@ -79,7 +79,7 @@ FILTERS = [dict(), dict(temperature=0.7), dict(temperature=0.0), dict(top_k=1), 
            dict(top_p=0.9), dict(top_p=1e-6), dict(temperature=1.5, top_p=0.999), dict(min_p=0.1), dict(min_p=1.0),
            dict(min_p=1e-7), dict(top_k=40, top_p=0.8), dict(top_k=300, top_p=0.95, min_p=0.001),
            dict(top_p=0.99, min_p=0.02), dict(top_k=10 ** 9), dict(top_k=100, min_p=0.3)]
-SIZES = [1, 2, 5, 127, 1000, SEG - 1, SEG, SEG + 1, 50257]
+SIZES = [1, 2, 5, 127, 1000, SEG - 1, SEG, SEG + 1, 2 * SEG, 50257]
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
