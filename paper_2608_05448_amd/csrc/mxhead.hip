@@ -20,6 +20,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+#include <utility>
+
 #include "gemm.hpp"
 #include "kernels.hpp"
 
@@ -35,33 +38,70 @@ __device__ __forceinline__ void lds_dma4_wait(const uint8_t* sbase, uint32_t vof
   asm volatile("s_nop 4\n\tglobal_load_lds_dword %0, %1" ::"v"(voff), "s"(sbase), "{m0}"(m0v) : "memory");
 }
 
+// A wave-uniform address in scalar registers, whatever the compiler has kept it in.
+template <class T>
+__device__ __forceinline__ const T* uniform(const T* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(u)));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(static_cast<uint32_t>(u >> 32)));
+  return reinterpret_cast<const T*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// For the kernel's lambdas: one that is left a call keeps the accumulators in memory.
+#define MX_INLINE __attribute__((always_inline))
+
+// f(0), ..., f(N - 1), each with a constant.
+template <class F, int... I>
+__device__ __forceinline__ void constant_for_each(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void constant_for(F&& f) {
+  constant_for_each(static_cast<F&&>(f), std::make_integer_sequence<int, N>{});
+}
+
 enum MxEpi : int { kMxLogits32 = 0, kMxLogits16 = 1, kMxHead = 2, kMxHeadArgmax = 3 };
 
-// BV x BM: vocabulary and state rows of a workgroup, WV x WM waves of 128 x (BM / WM) each. A stage is 128
-// values of every row (64 bytes in 4 bits, 128 in 8) and their scales, copied global -> LDS S - 1 stages
-// ahead into a ring of S.
-template <int HB_, int BV_, int BM_, int WV_, int WM_, int S_>
+// WV x WM waves, each with a vocabulary tile of 128 ids and 32 NCB states. A stage is 64 KS values of every row,
+// copied global -> LDS ahead into a ring of S. The scales come in groups of 512 values (G4; 16 bytes of a row at
+// a time: a copy of 64 rows touches 64 cache lines, however little it takes from each) or, where 512 does not
+// divide the padded row, 128 (KS = 2), into a ring of their own.
+template <int HB_, int WV_, int WM_, int NCB_, int KS_, int S_, bool G4_>
 struct MxCfg {
-  static constexpr int HB = HB_, BV = BV_, BM = BM_, WV = WV_, WM = WM_, S = S_;
+  static constexpr int HB = HB_, WV = WV_, WM = WM_, NCB = NCB_, KS = KS_, S = S_;
+  static constexpr bool G4 = G4_;
   static constexpr int NW = WV * WM, kThreads = 64 * NW;
-  static constexpr int NRB = 4, TM = BM / WM, NCB = TM / 32;
-  static constexpr int ROWA = 64, ROWB = 16 * HB;             // bytes of a row and stage
+  static constexpr int NRB = 4, TM = 32 * NCB, BV = 128 * WV, BM = TM * WM;
+  static constexpr int ROWA = 32 * KS, ROWB = 8 * HB * KS;    // bytes of a row and stage
+  static constexpr int CPA = ROWA / 16, CPB = ROWB / 16;      // its 16-byte chunks
   static constexpr int SB = (BM + 63) / 64 * 64;              // rows of h's scales, in whole copies
-  static constexpr int OFFB = BV * ROWA, OFFS = OFFB + BM * ROWB;
-  static constexpr int STAGE = OFFS + 4 * (BV + SB);
-  static constexpr int AW = BV / 16 / NW;                     // copies of a wave and stage: w rows,
-  static constexpr int BW = BM * ROWB / 1024 / NW;            // h rows,
-  static constexpr int SI = (BV + SB) / 64, SW = (SI + NW - 1) / NW;  // scales (some of them twice)
-  static constexpr int PER = AW + BW + SW;
-  static constexpr int kRing = S * STAGE, kStore = 16384 * NW;  // the epilogue's share of the same memory
+  static constexpr int GB = G4 ? 16 : 4;                      // bytes of a row's scales in a group
+  static constexpr int SPG = GB / (2 * KS);                   // stages of a group
+  static constexpr int OFFB = BV * ROWA, STAGE = OFFB + BM * ROWB;
+  static constexpr int NG = SPG == 1 ? S : 2;                 // groups in LDS
+  static constexpr int GROUP = GB * (BV + SB), OFFS = S * STAGE;
+  static constexpr int AI = BV * ROWA / 1024, AW = AI / NW;   // copies of a stage, and of a wave: w rows,
+  static constexpr int BI = BM * ROWB / 1024, BW = (BI + NW - 1) / NW;  // h rows (some of them twice),
+  static constexpr int SI = (BV + SB) / 64, SW = (SI + NW - 1) / NW;    // scales (some of them twice)
+  static constexpr int PER = AW + BW;
+  static constexpr int kRing = OFFS + NG * GROUP, kStore = 16384 * NW;  // the epilogue's share of the same memory
   static constexpr int kLds = kRing > kStore ? kRing : kStore;
   static constexpr int kWgPerCu = 160 * 1024 / kLds;
-  static constexpr int kWavesPerEu = kWgPerCu * NW < 8 ? 1 : 2;
-  static_assert(BV == 128 * WV && TM % 32 == 0, "a wave has a vocabulary tile");
-  static_assert(BV / 16 % NW == 0 && BM * ROWB / 1024 % NW == 0 && BW >= 1, "whole copies");
+  static constexpr int kWavesPerEu = kWgPerCu * NW < 8 || NCB > 2 ? 1 : 2;
+  static_assert(AI % NW == 0 && BI >= 1, "whole copies");
+  static_assert(KS == 2 || (KS == 4 && G4), "whole groups of stages");
+  static_assert(SPG == 1 || S <= SPG, "the ring's stages are of two groups at most");
   static_assert(S >= 2 && (S - 1) * PER <= 63, "ring depth and vmcnt range");
   static_assert(kLds <= 160 * 1024, "LDS per CU");
 };
+
+// Place of 16-byte chunk c of row r in a row of CP chunks in LDS, so that 16 lanes reading a chunk each of
+// consecutive rows meet all 64 banks.
+template <int CP>
+__device__ __forceinline__ int chunk_swz(int r) {
+  if constexpr (CP == 16) return r & 15;
+  else return dma_swz<CP>(r);
+}
 
 // Logits of a wave's 128 ids x 32 NCB states through LDS (16 KB of this wave, 8 for bf16), so that a store
 // instruction writes whole segments of a row, as in tile_logsoftmax_store_lds.
@@ -147,6 +187,8 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void mx_product_kernel
     const uint8_t* __restrict__ ws, void* __restrict__ logits, float* __restrict__ tls,
     float* __restrict__ lmass, uint64_t* __restrict__ amax, int64_t M, int64_t V, int dp, int n_mtiles) {
   constexpr int NRB = C::NRB, NCB = C::NCB, HB = C::HB;
+  // The weight's copies are non-temporal where no other workgroup reads them at about the same time.
+  constexpr bool kStream = C::NCB * C::WM <= 2;
   constexpr bool kSplit = HB == 8 && EPI != kMxLogits16;
   __shared__ __attribute__((aligned(1024))) char smem[C::kLds];
   const int tid = threadIdx.x;
@@ -159,22 +201,22 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void mx_product_kernel
   const int64_t m0 = static_cast<int64_t>(mt) * C::BM;
   const int64_t nv = V - v0, nm = M - m0;  // rows there are from here on; past them the last one repeats
 
-  // Copies. A row of a stage is 4 chunks of 16 bytes (8 of an 8-bit h), stored in another order by row.
+  // Copies. The 16-byte chunks of a row lie in another order by row.
   const int64_t pa = dp / 2, pb = dp / 8 * HB, ps = dp / 32;  // bytes of a row
-  const char* const srcA = reinterpret_cast<const char*>(w) + v0 * pa;
-  const char* const srcB = reinterpret_cast<const char*>(h) + m0 * pb;
-  const uint8_t* const srcS[2] = {ws + v0 * ps, hs + m0 * ps};
-  constexpr int CPB = C::ROWB / 16, RPB = 64 / CPB;  // chunks of an h row, rows of a copy
+  const char* const srcA = uniform(reinterpret_cast<const char*>(w) + v0 * pa);
+  const char* const srcB = uniform(reinterpret_cast<const char*>(h) + m0 * pb);
+  const uint8_t* const srcS[2] = {uniform(ws + v0 * ps), uniform(hs + m0 * ps)};
+  constexpr int CPA = C::CPA, CPB = C::CPB, RPA = 64 / CPA, RPB = 64 / CPB;  // chunks of a row, rows of a copy
   uint32_t offA[C::AW], offB[C::BW], offS[C::SW];
 #pragma unroll
   for (int i = 0; i < C::AW; ++i) {
-    const int r = (wave * C::AW + i) * 16 + lane / 4;
-    offA[i] = static_cast<uint32_t>((r < nv ? r : nv - 1) * pa + ((lane % 4) ^ dma_swz<4>(r)) * 16);
+    const int r = (wave * C::AW + i) * RPA + lane / CPA;
+    offA[i] = static_cast<uint32_t>((r < nv ? r : nv - 1) * pa + ((lane % CPA) ^ chunk_swz<CPA>(r)) * 16);
   }
 #pragma unroll
   for (int i = 0; i < C::BW; ++i) {
-    const int r = (wave * C::BW + i) * RPB + lane / CPB;
-    offB[i] = static_cast<uint32_t>((r < nm ? r : nm - 1) * pb + ((lane % CPB) ^ dma_swz<CPB>(r)) * 16);
+    const int r = (wave + i * C::NW) % C::BI * RPB + lane / CPB;
+    offB[i] = static_cast<uint32_t>((r < nm ? r : nm - 1) * pb + ((lane % CPB) ^ chunk_swz<CPB>(r)) * 16);
   }
 #pragma unroll
   for (int i = 0; i < C::SW; ++i) {
@@ -184,19 +226,32 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void mx_product_kernel
     offS[i] = static_cast<uint32_t>((r < n ? r : n - 1) * ps);
   }
   const uint32_t lds0 = lds_addr(smem);
-  auto copy = [&](int s, int slot) {
+  // Copy i of the kCopies that a wave makes for a stage, of stage s to ring slot `slot`: the scales, if a group
+  // begins with it, so that waiting for all but later stages' data waits for these, too; w; h. The stages of a copy
+  // come in order, and its offset moves on from one to the next.
+  constexpr int kCopies = C::SW + C::AW + C::BW;
+  auto copy = [&](auto i_, int s, int slot, auto group) MX_INLINE {
+    constexpr int i = decltype(i_)::value;
     const uint32_t to = lds0 + slot * C::STAGE;
-    const int64_t at = static_cast<int64_t>(s) * C::ROWA, bt = static_cast<int64_t>(s) * C::ROWB;
-#pragma unroll
-    for (int i = 0; i < C::AW; ++i)
-      lds_dma16_wait<true>(srcA + at, offA[i], to + (wave * C::AW + i) * 1024);
-#pragma unroll
-    for (int i = 0; i < C::BW; ++i)
-      lds_dma16_wait<false>(srcB + bt, offB[i], to + C::OFFB + (wave * C::BW + i) * 1024);
-#pragma unroll
-    for (int i = 0; i < C::SW; ++i) {
-      const int g = (wave + i * C::NW) % C::SI;
-      lds_dma4_wait(srcS[g < C::BV / 64 ? 0 : 1] + 4 * s, offS[i], to + C::OFFS + g * 256);
+    if constexpr (i < C::SW) {
+      if (group) {
+        const int at = (wave + i * C::NW) % C::SI;
+        const uint8_t* const from = uniform(at < C::BV / 64 ? srcS[0] : srcS[1]);
+        const uint32_t into = lds0 + C::OFFS + s / C::SPG % C::NG * C::GROUP + at * 64 * C::GB;
+        if constexpr (C::G4)
+          lds_dma16_wait<false>(reinterpret_cast<const char*>(from), offS[i], into);
+        else
+          lds_dma4_wait(from, offS[i], into);
+        offS[i] += C::GB;
+      }
+    } else if constexpr (i < C::SW + C::AW) {
+      constexpr int a = i - C::SW;
+      lds_dma16_wait<kStream>(srcA, offA[a], to + (wave * C::AW + a) * 1024);
+      offA[a] += C::ROWA;
+    } else {
+      constexpr int b = i - C::SW - C::AW;
+      lds_dma16_wait<false>(srcB, offB[b], to + C::OFFB + (wave + b * C::NW) % C::BI * 1024);
+      offB[b] += C::ROWB;
     }
   };
 
@@ -209,88 +264,183 @@ __global__ __launch_bounds__(C::kThreads, C::kWavesPerEu) void mx_product_kernel
       for (int r = 0; r < 16; ++r) acc[rb][cb][r] = 0.0f;
 
   const int lr = lane & 31, half = lane >> 5;
-  const int ta = dma_swz<4>(lr), tb = dma_swz<CPB>(lr);  // the same for every block of 32 rows
+  const int ta = chunk_swz<CPA>(lr), tb = chunk_swz<CPB>(lr);  // the same for every block of 32 rows
   const int a_base = (wv * kVTile + lr) * C::ROWA;
   const int b_base = C::OFFB + (wm * C::TM + lr) * C::ROWB;
-  const int sa_base = C::OFFS + (wv * kVTile + lr) * 4;
-  const int sb_base = C::OFFS + (C::BV + wm * C::TM + lr) * 4;
-  const int nk = dp / kMxPad;
-#pragma unroll
-  for (int j = 0; j < C::S - 1; ++j)
-    if (j < nk) copy(j, j);
-  int slot = 0;
-  for (int kt = 0; kt < nk; ++kt) {
-    // Stages kt + 1 .. kt + S - 2 may still be in flight; near the end all have to be in.
-    if (kt + C::S - 1 <= nk)
-      wait_vmcnt<(C::S - 2) * C::PER>();
-    else
-      wait_vmcnt<0>();
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    // Every wave has read stage kt - 1: its slot takes stage kt + S - 1.
-    if (kt + C::S - 1 < nk) copy(kt + C::S - 1, slot == 0 ? C::S - 1 : slot - 1);
-    const char* base = smem + slot * C::STAGE;
-    // The bytes of this lane's scales: 0 of the first step and 2 of the second.
-    int sa[NRB], sb[NCB];
+  const int sa_base = (wv * kVTile + lr) * C::GB;
+  const int sb_base = (C::BV + wm * C::TM + lr) * C::GB;
+  const int nk = dp / (64 * C::KS);
+  // Fragments of two 64-deep steps, the one that is computed and the next one's, by its parity.
+  i32x8 af[2][NRB], bf[2][NCB];
+  // Read i of the kReads of a step's fragments, in the order in which the products need them.
+  constexpr int kReads = NRB + NCB;
+  auto read = [&](auto i_, const char* base, auto ks_) MX_INLINE {
+    constexpr int i = decltype(i_)::value, ks = decltype(ks_)::value, p = ks & 1;
+    if constexpr (i >= 1 && i <= NRB) {
+      constexpr int rb = i - 1;
+      const i32x4 x = *reinterpret_cast<const i32x4*>(base + a_base + rb * 32 * C::ROWA + (((2 * ks + half) ^ ta) * 16));
+      af[p][rb] = __builtin_shufflevector(x, i32x4{}, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      constexpr int cb = i == 0 ? 0 : i - NRB;
+      const char* row = base + b_base + cb * 32 * C::ROWB;
+      if constexpr (HB == 4) {
+        const i32x4 x = *reinterpret_cast<const i32x4*>(row + (((2 * ks + half) ^ tb) * 16));
+        bf[p][cb] = __builtin_shufflevector(x, i32x4{}, 0, 1, 2, 3, 4, 5, 6, 7);
+      } else {
+        const i32x4 x = *reinterpret_cast<const i32x4*>(row + (((4 * ks + half) ^ tb) * 16));
+        const i32x4 y = *reinterpret_cast<const i32x4*>(row + (((4 * ks + 2 + half) ^ tb) * 16));
+        bf[p][cb] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    }
+  };
+  // A stage's scales: words of two steps each, of which bytes 0 and 2 are this lane's after the shift.
+  constexpr int SWD = C::KS / 2;
+  struct Scales {
+    int a[SWD][NRB], b[SWD][NCB];
+  };
+  Scales sc, next;
+  auto load_scales = [&](int s, Scales& to) MX_INLINE {
+    const char* base = smem + C::OFFS + s / C::SPG % C::NG * C::GROUP + s % C::SPG * (2 * C::KS);
 #pragma unroll
     for (int rb = 0; rb < NRB; ++rb)
-      sa[rb] = static_cast<int>(*reinterpret_cast<const uint32_t*>(base + sa_base + rb * 128) >> (8 * half));
+#pragma unroll
+      for (int i = 0; i < SWD; ++i)
+        to.a[i][rb] = *reinterpret_cast<const int*>(base + sa_base + rb * 32 * C::GB + 4 * i);
 #pragma unroll
     for (int cb = 0; cb < NCB; ++cb)
-      sb[cb] = static_cast<int>(*reinterpret_cast<const uint32_t*>(base + sb_base + cb * 128) >> (8 * half));
-    auto step = [&](auto ks_) {
-      constexpr int ks = decltype(ks_)::value;
-      i32x8 af[NRB], bf[NCB];
 #pragma unroll
-      for (int rb = 0; rb < NRB; ++rb) {
-        const i32x4 x = *reinterpret_cast<const i32x4*>(base + a_base + rb * 32 * C::ROWA +
-                                                        (((2 * ks + half) ^ ta) * 16));
-        af[rb] = __builtin_shufflevector(x, i32x4{}, 0, 1, 2, 3, 4, 5, 6, 7);
-      }
+      for (int i = 0; i < SWD; ++i)
+        to.b[i][cb] = *reinterpret_cast<const int*>(base + sb_base + cb * 32 * C::GB + 4 * i);
+  };
+  auto take_scales = [&](const Scales& from) MX_INLINE {
 #pragma unroll
-      for (int cb = 0; cb < NCB; ++cb) {
-        const char* row = base + b_base + cb * 32 * C::ROWB;
-        if constexpr (HB == 4) {
-          const i32x4 x = *reinterpret_cast<const i32x4*>(row + (((2 * ks + half) ^ tb) * 16));
-          bf[cb] = __builtin_shufflevector(x, i32x4{}, 0, 1, 2, 3, 4, 5, 6, 7);
-        } else {
-          const i32x4 x = *reinterpret_cast<const i32x4*>(row + (((4 * ks + half) ^ tb) * 16));
-          const i32x4 y = *reinterpret_cast<const i32x4*>(row + (((4 * ks + 2 + half) ^ tb) * 16));
-          bf[cb] = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-      }
-      constexpr int fmt = HB == 4 ? 4 : 0;
+    for (int i = 0; i < SWD; ++i) {
 #pragma unroll
-      for (int cb = 0; cb < NCB; ++cb) {
-        if constexpr (kSplit) {
-          i32x8 large, small;
+      for (int rb = 0; rb < NRB; ++rb) sc.a[i][rb] = from.a[i][rb] >> (8 * half);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const uint32_t m = large_codes(static_cast<uint32_t>(bf[cb][i]));
-            large[i] = bf[cb][i] & static_cast<int>(m);
-            small[i] = bf[cb][i] & static_cast<int>(~m);
+      for (int cb = 0; cb < NCB; ++cb) sc.b[i][cb] = from.b[i][cb] >> (8 * half);
+    }
+  };
+  // A step, and other(n) after its product n. A product takes the matrix pipe for 32 cycles (64 with an 8-bit h), and
+  // the wave issues in order: what it does besides (LDS reads, copies) goes a little at a time between products, since
+  // a burst of it leaves the pipe empty, with one wave to a SIMD.
+  constexpr int kProducts = NRB * NCB;
+  auto step = [&](auto ks_, auto other) MX_INLINE {
+    constexpr int ks = decltype(ks_)::value, p = ks & 1, fmt = HB == 4 ? 4 : 0, i = ks / 2, op = 2 * (ks & 1);
+    i32x8 large, small;
+    constant_for<kProducts>([&](auto n_) MX_INLINE {
+      constexpr int n = decltype(n_)::value, cb = n / NRB, rb = n % NRB;
+      if constexpr (kSplit) {
+        if constexpr (rb == 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t m = large_codes(static_cast<uint32_t>(bf[p][cb][e]));
+            large[e] = bf[p][cb][e] & static_cast<int>(m);
+            small[e] = bf[p][cb][e] & static_cast<int>(~m);
           }
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb)
-            acc[rb][cb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                af[rb], small, acc[rb][cb], 4, fmt, 2 * ks, sa[rb], 2 * ks, sb[cb]);
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb)
-            acc[rb][cb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                af[rb], large, acc[rb][cb], 4, fmt, 2 * ks, sa[rb], 2 * ks, sb[cb]);
-        } else {
-#pragma unroll
-          for (int rb = 0; rb < NRB; ++rb)
-            acc[rb][cb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
-                af[rb], bf[cb], acc[rb][cb], 4, fmt, 2 * ks, sa[rb], 2 * ks, sb[cb]);
         }
+        acc[rb][cb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            af[p][rb], small, acc[rb][cb], 4, fmt, op, sc.a[i][rb], op, sc.b[i][cb]);
+        acc[rb][cb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            af[p][rb], large, acc[rb][cb], 4, fmt, op, sc.a[i][rb], op, sc.b[i][cb]);
+      } else {
+        acc[rb][cb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+            af[p][rb], bf[p][cb], acc[rb][cb], 4, fmt, op, sc.a[i][rb], op, sc.b[i][cb]);
       }
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
-    slot = slot + 1 == C::S ? 0 : slot + 1;
-  }
+      __builtin_amdgcn_sched_barrier(0);
+      other(n_);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+  };
+  // f(i) for those of `count` things that come after product n, if they are spread over the first `over` products.
+  auto spread = [&](auto n_, auto count_, auto over_, auto f) MX_INLINE {
+    constexpr int n = decltype(n_)::value, count = decltype(count_)::value, over = decltype(over_)::value;
+    constant_for<count>([&](auto i_) MX_INLINE {
+      if constexpr (decltype(i_)::value * over / count == n) f(i_);
+    });
+  };
+  // The next step's fragments: all under way before the last products, which cover their latency.
+  constexpr std::integral_constant<int, kReads> reads{};
+  constexpr std::integral_constant<int, (kProducts * 3 + 3) / 4> early{};
+  // The copies of a stage go into kCopySteps steps: the last one of stage s - S, whose slot they take, and the
+  // first ones of the stage after that, as long as a step is left before they are waited for.
+  constexpr int kCopySteps = C::S > 2 ? C::KS : C::KS - 1;
+  auto copies = [&](auto n_, auto step_, int s, int slot, auto group) MX_INLINE {
+    constexpr int from = (decltype(step_)::value * kCopies + kCopySteps - 1) / kCopySteps;
+    constexpr int to = ((decltype(step_)::value + 1) * kCopies + kCopySteps - 1) / kCopySteps;
+    if constexpr (decltype(step_)::value < kCopySteps && to > from)
+      spread(n_, std::integral_constant<int, to - from>{}, std::integral_constant<int, kProducts>{},
+             [&](auto i_) MX_INLINE { copy(std::integral_constant<int, from + decltype(i_)::value>{}, s, slot, group); });
+  };
+
+  // Prologue: the ring in flight, of the last stage in it what the last step of the one before the first would start.
+  constexpr int kFirst = (kCopies + kCopySteps - 1) / kCopySteps;  // copies of a stage in its first step
+#pragma unroll
+  for (int j = 0; j < C::S; ++j)
+    if (j < nk)
+      constant_for<kCopies>([&](auto i_) MX_INLINE {
+        if (j + 1 < C::S || decltype(i_)::value < kFirst) copy(i_, j, j, j % C::SPG == 0);
+      });
+  if (nk >= C::S)
+    wait_vmcnt<(C::S - 2) * C::PER + (kFirst > C::SW ? kFirst - C::SW : 0)>();
+  else
+    wait_vmcnt<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  constant_for<kReads>([&](auto i_) MX_INLINE { read(i_, smem, std::integral_constant<int, 0>{}); });
+  load_scales(0, next);
+  // A wave reads its fragments a step before it needs them. So before the last step of a stage every wave has all of
+  // it in registers, and the barrier that lies there (each wave has waited for its own copies of the next
+  // stage) both opens the next stage and frees this one's slot, for the copies of stage kt + S.
+  // late: the rest of the copies of stage kt + S - 1; more: a stage follows; begin: stage kt + S is there; now, then:
+  // whether a group of scales begins with those two. Constants in the main part of the loop: around a branch the
+  // compiler moves the products away from what is to run beside them.
+  int slot = 0;
+  auto stage = [&](int kt, auto late, auto more, auto begin, auto now, auto then) MX_INLINE {
+    const char* const base = smem + slot * C::STAGE;
+    take_scales(next);
+    const int before = slot == 0 ? C::S - 1 : slot - 1;
+    constant_for<C::KS - 1>([&](auto ks_) MX_INLINE {
+      constexpr int ks = decltype(ks_)::value;
+      step(ks_, [&](auto n_) MX_INLINE {
+        spread(n_, reads, early, [&](auto i_) MX_INLINE { read(i_, base, std::integral_constant<int, ks + 1>{}); });
+        if (late) copies(n_, std::integral_constant<int, ks + 1>{}, kt + C::S - 1, before, now);
+      });
+    });
+    const int after = slot + 1 == C::S ? 0 : slot + 1;
+    if (more) {
+      // Stages kt + 2 .. kt + S - 1 may still be in flight; near the end all have to be in.
+      if (begin || C::S == 2)
+        wait_vmcnt<(C::S - 2) * C::PER>();
+      else
+        wait_vmcnt<0>();
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    }
+    step(std::integral_constant<int, C::KS - 1>{}, [&](auto n_) MX_INLINE {
+      if (more) {
+        spread(n_, reads, early,
+               [&](auto i_) MX_INLINE { read(i_, smem + after * C::STAGE, std::integral_constant<int, 0>{}); });
+        if constexpr (decltype(n_)::value == 0) load_scales(kt + 1, next);
+      }
+      if (begin) copies(n_, std::integral_constant<int, 0>{}, kt + C::S, slot, then);
+    });
+    slot = after;
+  };
+  const std::true_type yes{};
+  const std::false_type no{};
+  int kt = 0;
+  for (; kt + C::S + C::SPG - 1 < nk; kt += C::SPG)
+    constant_for<C::SPG>([&](auto g_) MX_INLINE {
+      constexpr int g = decltype(g_)::value;
+      stage(kt + g, yes, yes, yes, std::integral_constant<bool, (g + C::S - 1) % C::SPG == 0>{},
+            std::integral_constant<bool, (g + C::S) % C::SPG == 0>{});
+    });
+  for (; kt + C::S < nk; ++kt) stage(kt, yes, yes, yes, (kt + C::S - 1) % C::SPG == 0, (kt + C::S) % C::SPG == 0);
+  if (kt + 1 < nk && kt + C::S - 1 < nk) stage(kt, yes, yes, no, (kt + C::S - 1) % C::SPG == 0, no), ++kt;
+  for (; kt + 1 < nk; ++kt) stage(kt, no, yes, no, no, no);
+  stage(kt, no, no, no, no, no);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __builtin_amdgcn_s_barrier();  // the ring is free: nothing reads it, every copy has landed
   asm volatile("" ::: "memory");
@@ -316,10 +466,35 @@ hipError_t launch_as(const MxProductArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+#ifndef MXA
+#define MXA 2, 1, 1, 2, 2, true
+#endif
+#ifndef MXB
+#define MXB 2, 2, 1, 2, 3, true
+#endif
+#ifndef MXC
+#define MXC 2, 2, 2, 2, 3, true
+#endif
+#ifndef MXD4
+#define MXD4 2, 2, 4, 4, 2, true
+#endif
+#ifndef MXD8
+#define MXD8 2, 2, 4, 2, 2, true
+#endif
 template <int HB, int EPI>
 hipError_t launch_bits(const MxProductArgs& a, hipStream_t stream) {
-  if (a.M <= 64) return launch_as<MxCfg<HB, 256, 64, 2, 2, 3>, EPI>(a, stream);
-  return launch_as<MxCfg<HB, 256, 128, 2, 2, HB == 4 ? 3 : 2>, EPI>(a, stream);
+  if (a.dp % 512 == 0) {
+    if (a.M <= 32) return launch_as<MxCfg<HB, MXA>, EPI>(a, stream);
+    if (a.M <= 64) return launch_as<MxCfg<HB, MXB>, EPI>(a, stream);
+    if (a.M <= 128) return launch_as<MxCfg<HB, MXC>, EPI>(a, stream);
+    if constexpr (HB == 8) {
+      return launch_as<MxCfg<HB, MXD8>, EPI>(a, stream);
+    } else {
+      return launch_as<MxCfg<HB, MXD4>, EPI>(a, stream);
+    }
+  }
+  if (a.M <= 64) return launch_as<MxCfg<HB, 2, 2, 1, 2, 3, false>, EPI>(a, stream);
+  return launch_as<MxCfg<HB, 2, 2, 2, 2, 3, false>, EPI>(a, stream);
 }
 
 template <int EPI>
