@@ -466,35 +466,27 @@ hipError_t launch_as(const MxProductArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-#ifndef MXA
-#define MXA 2, 1, 1, 2, 2, true
-#endif
-#ifndef MXB
-#define MXB 2, 2, 1, 2, 3, true
-#endif
-#ifndef MXC
-#define MXC 2, 2, 2, 2, 3, true
-#endif
-#ifndef MXD4
-#define MXD4 2, 2, 4, 4, 2, true
-#endif
-#ifndef MXD8
-#define MXD8 2, 2, 4, 2, 2, true
-#endif
+// Tiles, us by (ids x states, values of a stage, waves a CU) at V = 151,936: 17 states of 8 bits at d = 2560 60 with
+// 256 x 64, 256 deep, 61 with 256 x 32, 256 deep, 73 with 256 x 32, 128 deep, 94 with 512 x 32. 272 states of 8 bits
+// at d = 4096, bf16 logits: 193 with 256 x 128, 128 deep, two workgroups to a CU, 220 with one of three stages, 214
+// with 256 x 192, 256 with 256 x 256. 2048 states of 4 bits at d = 4096, the head's form: 841 with 256 x 256,
+// 256 deep (128 x 128 a wave), 862 with 128 deep, 857 with eight waves of 128 x 64, 1004 with 256 x 128, two
+// workgroups to a CU. Of an 8-bit h a product takes twice as long, and the second workgroup, which hides the
+// first one's stores, is worth more than the larger tile.
 template <int HB, int EPI>
 hipError_t launch_bits(const MxProductArgs& a, hipStream_t stream) {
-  if (a.dp % 512 == 0) {
-    if (a.M <= 32) return launch_as<MxCfg<HB, MXA>, EPI>(a, stream);
-    if (a.M <= 64) return launch_as<MxCfg<HB, MXB>, EPI>(a, stream);
-    if (a.M <= 128) return launch_as<MxCfg<HB, MXC>, EPI>(a, stream);
-    if constexpr (HB == 8) {
-      return launch_as<MxCfg<HB, MXD8>, EPI>(a, stream);
-    } else {
-      return launch_as<MxCfg<HB, MXD4>, EPI>(a, stream);
-    }
+  if (a.dp % 512 != 0) {
+    if (a.M <= 64) return launch_as<MxCfg<HB, 2, 2, 1, 2, 3, false>, EPI>(a, stream);
+    return launch_as<MxCfg<HB, 2, 2, 2, 2, 3, false>, EPI>(a, stream);
   }
-  if (a.M <= 64) return launch_as<MxCfg<HB, 2, 2, 1, 2, 3, false>, EPI>(a, stream);
-  return launch_as<MxCfg<HB, 2, 2, 2, 2, 3, false>, EPI>(a, stream);
+  if (a.M <= 64) return launch_as<MxCfg<HB, 2, 2, 1, 4, 2, true>, EPI>(a, stream);
+  if constexpr (HB == 4) {
+    // In rounds of the GPU, one workgroup to a CU or two: a round of the larger tiles takes 0.84 of one of the others.
+    const int64_t vt = (a.V + 255) / 256;
+    const int64_t large = (vt * ((a.M + 255) / 256) + 255) / 256, small = (vt * ((a.M + 127) / 128) + 511) / 512;
+    if (a.M > 128 && 84 * large <= 100 * small) return launch_as<MxCfg<HB, 2, 2, 4, 4, 2, true>, EPI>(a, stream);
+  }
+  return launch_as<MxCfg<HB, 2, 2, 2, 2, 2, true>, EPI>(a, stream);
 }
 
 template <int EPI>

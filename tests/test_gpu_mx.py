@@ -247,7 +247,8 @@ def _logit_bound(hd, wd, bits, dtype):
 
 
 SHAPES = [(1, 1, 1), (1, 5, 64), (3, 127, 33), (17, 1000, 200), (32, 129, 128), (33, 256, 512), (64, 1001, 1000),
-          (65, 640, 96), (128, 300, 256), (129, 2049, 384), (260, 515, 1024), (5, 50257, 64)]
+          (65, 640, 96), (128, 300, 256), (129, 2049, 384), (260, 515, 1024), (5, 50257, 64),
+          (513, 33000, 512), (70, 400, 2560)]
 
 
 @pytest.mark.parametrize("bits", [4, 8])
