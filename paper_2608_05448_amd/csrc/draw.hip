@@ -10,10 +10,11 @@
 // kDrawSeg ids, and about 2048 workgroups share the segments of all rows, so that few rows still use the whole
 // GPU. Workgroups of a row meet at the ends of launches only: an agent-wide fence per workgroup, for
 // a counter that lets the last one go on, writes back and empties an L2 each time (1024 rows of 50,257 ids
-// took 2,080 us that way). The launches after the first read the logits from the caches:
+// took 2,080 us that way, 82 now). The launches after the first read the logits from the caches:
 //   top     maximum of each part of a row, and of each 128 ids
 //   bins    without filters the sum of each segment's weights; under top-p alone (or with min-p), masses in
 //           bins of max - s; under a top-k past the number of 128s, counts
+//   find    (only where there are filters) a workgroup per row finds the cut's bound, as follows
 //   cut     (only where there are filters) lists the ids that the cut goes through, and sums by segment what is
 //           surely kept. Top-k: the k-th largest of the maxima of 128 ids is a bound from below for the k-th
 //           largest id, so that what reaches it holds all that is kept (about k ids) and nothing else
@@ -21,6 +22,8 @@
 //   finish  a workgroup per row: sorts the list, finds the exact cut and draws. Rows whose list is
 //           longer than kListMost (many equal logits), or with a large top-k and top-p at once, are selected by
 //           radix over their order-preserving keys here
+// 272 rows of 151,936 ids under parameters of their own 133 us (top 38, bins 28, find 9, cut 31, finish 29; reading them
+// once takes 24.5), one under a nucleus 31. A weight costs 33 vector operations, which bounds bins and cut.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
