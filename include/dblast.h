@@ -594,9 +594,9 @@ dbl_status dbl_mx_head_logprobs(dbl_shape shape, int bits, const void* h, const 
  * A row without a distribution (parameters of its arrays out of range, a NaN among its logits, its
  * largest s infinite) gets token -1 and logprob NaN.
  *   ws        workspace of dbl_workspace_bytes(DBL_OP_SAMPLE_LOGITS, shape) bytes, shape.B * shape.K = N
- * token and logprob may overlap neither each other nor an input. Errors: DBL_EINVAL for null, misaligned or overlapping pointers
- * (arrays of a value per row need their elements' alignment only) or numbers out of range; DBL_EDTYPE;
- * DBL_ESHAPE; DBL_EWORKSPACE; DBL_EHIP (where a launch would need 2^32 threads).
+ * token and logprob may overlap neither each other nor an input. Errors: DBL_EINVAL for null, misaligned
+ * or overlapping pointers (arrays of a value per row need their elements' alignment only) or numbers out of
+ * range; DBL_EDTYPE; DBL_ESHAPE; DBL_EWORKSPACE; DBL_EHIP (where a launch would need 2^32 threads).
  */
 typedef struct {
   float temperature;

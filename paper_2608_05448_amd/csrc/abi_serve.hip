@@ -135,7 +135,7 @@ dbl_status dbl_mx_head_logprobs(dbl_shape s, int bits, const void* h, const uint
                                 void* ws_mem, size_t ws_bytes, void* stream) {
   return guarded([&]() -> dbl_status {
     if (dbl_status st = check_shape(s, true)) return st;
-    if (bits != 4 && bits != 8) return fail(DBL_EINVAL, "bits must be 4 or 8");
+    if (dbl_status st = check_rows(s.B * s.K * s.R, s.d, bits)) return st;
     if (s.B == 0) return ok();
     if (!h || !hs || !w || !ws || !tls || !lmass || !lse) return fail(DBL_EINVAL, "NULL pointer");
     if (dbl_status st = check_aligned({{h, "h"}, {hs, "hs"}, {w, "w"}, {ws, "ws"}, {tls, "tls"},
