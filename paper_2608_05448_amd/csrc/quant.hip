@@ -262,7 +262,7 @@ __global__ __launch_bounds__(256) void norm_kernel(const T* x, const T* residual
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const double p = static_cast<double>(v[i]) * scale * static_cast<double>(w[i]);
-      v[i] = round_odd(p);
+      v[i] = j < d ? round_odd(p) : 0.0f;  // padding is 0 also where the row's scale is infinite or NaN
       w[i] = sizeof(T) == 4 ? static_cast<float>(p) : v[i];
     }
     if (y) store8<T, VEC>(y + row * d, j, d, w);

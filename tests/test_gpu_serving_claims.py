@@ -1,6 +1,7 @@
 """What the low-precision serving operators state of themselves, at the places where it is decided: the norm's
-codes and y are those of the exact value, no product of 8-bit states is cut where the result is binary32, a
-row does not depend on the batch for any tile, and the draw over of more than 64 segments and of rows that the short lists cannot hold.
+codes and y are those of the exact value and its padding is what quantising y gives, no product of 8-bit states
+is cut where the result is binary32, a row does not depend on the batch for any tile, and the draw over more
+than 64 segments and of rows that its list does not hold.
 
 Bounds. The norm is computed in binary64 (half a step 2^-53): squares are exact (24 bits each), and are added
 8 ceil(dp / 2048) at a time in a register and then by 8 levels; after the root half of that error is left, and a
@@ -12,7 +13,7 @@ import pytest
 import torch
 
 from test_gpu_draw import check, rand_logits, rand_words
-from test_gpu_mx import _data, _operands, _table, _unpack, _values
+from test_gpu_mx import _operands, _table, _values
 
 pytestmark = pytest.mark.gpu
 
@@ -103,6 +104,31 @@ def test_norm_result_in_bf16_is_rounded_once():
     got = D.dbl_add_rmsnorm_mx(x.cuda(), None, w.cuda(), eps=1e-6, want_y=True)[3]
     got = got.cpu().double().numpy().astype(LD)
     assert np.array_equal(got[sure], once[sure])
+
+
+@pytest.mark.parametrize("bits", [8, 4])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [1, 33, 100, 200, 1000, 1001, 4104, 9000])
+def test_norm_padding_is_that_of_the_quantised_result(d, dtype, bits):
+    """Rows of zeros without eps, with NaN and with infinities have their padding as any other: code 0 under
+    the smallest scale, as quantising y gives it."""
+    from paper_2608_05448_amd import dblast as D
+    x = torch.randn((5, d), generator=torch.Generator().manual_seed(d))
+    x[0] = 0.0
+    x[1, d // 2] = float("nan")
+    x[2, d - 1] = float("inf")
+    x[3, 0] = -float("inf")
+    x = x.to(dtype).cuda()
+    w = torch.ones(d, dtype=dtype).cuda()
+    _, codes, scales, y = D.dbl_add_rmsnorm_mx(x, None, w, eps=0.0, bits=bits, want_y=True)
+    want = D.dbl_mx_quantize(y, bits=bits)
+    dp, blocks = D.mx_row(d), (d + 31) // 32
+    s = scales.view(torch.uint8).cpu()
+    assert s.shape == (5, dp // 32)
+    assert bool((s[:, blocks:] == 0).all()), "scale of a block of padding"
+    broken = want[1].view(torch.uint8).cpu() == 255
+    assert torch.equal(s == 255, broken)
+    assert bool((codes.view(torch.uint8).cpu()[:, blocks * 4 * bits:] == 0).all()), "codes of padding"
 
 
 @pytest.mark.parametrize("half", ["small", "large"])
