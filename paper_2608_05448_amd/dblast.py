@@ -822,6 +822,11 @@ def dbl_mx_head_logprobs(h, h_scales, w, w_scales, tls=None, lmass=None, lse=Non
     return (tls, lmass, lse, argmax) if want_arg else (tls, lmass, lse)
 
 
+def _whole(k):
+    """A whole number for a 64-bit field: past its range it keeps its sign and its size, not its low bits."""
+    return max(-(1 << 62), min(operator.index(k), 1 << 62))
+
+
 def dbl_sample_logits(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, token=None,
                       logprob=None, ws=None):
     """One token per row of logits [..., V] (fp32 or bf16) from random words [...] (int32, all 32 bits
@@ -838,7 +843,7 @@ def dbl_sample_logits(logits, words, temperature=1.0, top_k=0, top_p=1.0, min_p=
     p = Sampling(1.0, 1.0, 0.0, 0, None, None, None, None)
     given = {}
     for name, many, value, dtype, plain in (("temperature", "temperatures", temperature, torch.float32, float),
-                                            ("top_k", "top_ks", top_k, torch.int32, operator.index),
+                                            ("top_k", "top_ks", top_k, torch.int32, _whole),
                                             ("top_p", "top_ps", top_p, torch.float32, float),
                                             ("min_p", "min_ps", min_p, torch.float32, float)):
         if isinstance(value, torch.Tensor):

@@ -210,3 +210,16 @@ def test_draw_of_rows_that_the_list_does_not_hold():
         for f in [dict(top_k=50), dict(top_k=400, top_p=0.9), dict(top_k=1187), dict(top_k=1188), dict(top_k=1150, min_p=1e-4)]:
             print(f"[draw] ordered {x.dtype} {f}", flush=True)
             check(x, words, **f)
+
+
+def test_draw_takes_any_whole_number_as_top_k():
+    """0, or the vocabulary's size and more: off, also past 64 bits."""
+    from paper_2608_05448_amd import dblast as D
+    x, words = rand_logits(8, 3000, 1).cuda(), rand_words(8, 2).cuda()
+    want = D.dbl_sample_logits(x, words)
+    for k in (3000, 1 << 31, (1 << 32) + 1, (1 << 63) - 1, 1 << 63, (1 << 64) + 1):
+        got = D.dbl_sample_logits(x, words, top_k=k)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), k
+    for k in (-1, -(1 << 63) - 1, -(1 << 64) + 5):
+        with pytest.raises(D.DblastError):
+            D.dbl_sample_logits(x, words, top_k=k)
