@@ -693,6 +693,8 @@ def _mx_out(rows, d, bits, device, codes, scales):
 
 def _mx_in(codes, scales, name):
     """Leading shape, values of a padded row and bits of microscaled rows."""
+    if not isinstance(codes, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
     bits = _MX_BITS.get(codes.dtype)
     if bits is None:
         raise TypeError(f"{name} must be uint8 (4-bit codes) or float8_e4m3fn, got {codes.dtype}")
