@@ -515,6 +515,7 @@ dbl_status dbl_clip_grads(int64_t n, const void* const* grads, void* const* out,
  * Rounding: with E = 2 (4 bits) or 8, a block's scale is 2^(floor(log2 max|x|) - E), at least 2^-127, and
  * a value over it is rounded to the nearest code, ties to the even code, and to the largest one where it
  * is beyond it. A block that holds an infinity or NaN has scale 255 and codes 0: all its values are NaN.
+ * dbl_mx_row is 0 for d < 1 and where dp does not fit 64 bits.
  */
 int64_t dbl_mx_row(int64_t d);
 

@@ -58,7 +58,7 @@ dbl_status quantize(int64_t M, int64_t d, int dt, const void* x, int bits, const
 
 extern "C" {
 
-int64_t dbl_mx_row(int64_t d) { return d < 1 ? 0 : dbl::mx_row(d); }
+int64_t dbl_mx_row(int64_t d) { return d < 1 || d > INT64_MAX - 127 ? 0 : dbl::mx_row(d); }
 
 dbl_status dbl_mx_quantize(int64_t M, int64_t d, int dt, const void* x, int bits, void* codes,
                            uint8_t* scales, void* stream) {
