@@ -1707,17 +1707,23 @@ hipError_t launch_head_train(const HeadTrainArgs& a, bool grad, hipStream_t stre
 
 hipError_t launch_argmax_clear(uint64_t* amax, int64_t M, hipStream_t stream) {
   const int64_t zb = (M + 255) / 256;
-  if (zb > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (zb > kMaxThreads / 256) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(zero_u64_kernel, dim3(static_cast<unsigned>(zb)), dim3(256), 0, stream, amax, M);
   return hipGetLastError();
 }
 
 hipError_t launch_lse(const float* lmass, float* lse, const uint64_t* amax, int32_t* argmax, int64_t M,
                       int nT, hipStream_t stream) {
-  const int64_t lse_blocks = (M + 3) / 4;
-  hipLaunchKernelGGL(lse_finalize_kernel, dim3(static_cast<unsigned>(lse_blocks)), dim3(256), 0,
-                     stream, lmass, lse, amax, amax ? argmax : nullptr, M, nT);
-  return hipGetLastError();
+  // A wave per row: 2^26 rows are more threads than a launch has (and what is more is dropped without
+  // an error), so they are taken in pieces.
+  constexpr int64_t kMostRows = kMaxThreads / 256 * 4;
+  for (int64_t m = 0; m < M; m += kMostRows) {
+    const int64_t rows = M - m < kMostRows ? M - m : kMostRows;
+    hipLaunchKernelGGL(lse_finalize_kernel, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, stream,
+                       lmass + m * nT, lse + m, amax ? amax + m : nullptr, amax ? argmax + m : nullptr, rows, nT);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch_head(const HeadArgs& a, hipStream_t stream) {

@@ -223,3 +223,24 @@ def test_draw_takes_any_whole_number_as_top_k():
     for k in (-1, -(1 << 63) - 1, -(1 << 64) + 5):
         with pytest.raises(D.DblastError):
             D.dbl_sample_logits(x, words, top_k=k)
+
+
+@pytest.mark.parametrize("argmax", [False, True])
+def test_head_of_more_rows_than_a_launch_of_a_wave_each_takes(argmax):
+    """2^26 rows, a wave each, are 2^32 threads: more than one launch has. Rows around that place, the first and
+    the last ones are what a small call gives."""
+    from paper_2608_05448_amd import dblast as D
+    M, V = (1 << 26) + 205, 3
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = torch.empty((M, 64), dtype=torch.uint8, device="cuda").random_(0, 256, generator=g)
+    hs = torch.full((M, 4), 126, dtype=torch.uint8, device="cuda").view(torch.float8_e8m0fnu)
+    w, ws = D.dbl_mx_quantize(torch.randn((V, 128), generator=torch.Generator().manual_seed(2)).cuda())
+    lse = torch.full((M, 1, 1), float("nan"), device="cuda")
+    got = D.dbl_mx_head_logprobs(h.view(M, 1, 1, 64), hs.view(M, 1, 1, 4), w, ws, lse=lse, argmax=argmax)
+    assert not bool(torch.isnan(lse).any())
+    most = ((1 << 32) - 1) // 256 * 4
+    for a in (0, most - 50, M - 100):
+        want = D.dbl_mx_head_logprobs(h[a:a + 100].clone().view(100, 1, 1, 64), hs[a:a + 100].clone().view(100, 1, 1, 4),
+                                      w, ws, argmax=argmax)
+        for x, y in zip(got, want):
+            assert torch.equal(x[a:a + 100], y), a
