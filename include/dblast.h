@@ -74,7 +74,9 @@
  *    (within a call, every workspace word is written before it is read), so the calls may be
  *    captured into a HIP graph and replayed.
  *  - Errors: a non-zero dbl_status is returned before anything is launched when an argument is
- *    invalid; DBL_EHIP reports a failed launch. dbl_last_error() gives a message for the
+ *    invalid; DBL_EHIP reports a failed launch, and any call's launch that would need 2^32 threads
+ *    (2^24 blocks, positions or rows for most, 2^22 rows under filters in dbl_target_logprobs; the
+ *    head's rows are bound by its tiles alone). dbl_last_error() gives a message for the
  *    calling thread's last failure. Data-dependent problems (NaN inputs) are not detected.
  *  - Shapes: K, R, d, V >= 1, B >= 0 (B = 0 is a no-op), R <= 64, V < 2^24, d <= 2^20 and
  *    d % 8 == 0 for the bf16 head, M * V < 2^62.

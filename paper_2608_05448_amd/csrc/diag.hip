@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kProbeThreads) void read_probe_kernel(const float4*
 
 hipError_t launch_read_probe(const void* buf, int64_t bytes, float* partials, int64_t n_partials,
                              hipStream_t stream) {
-  if (n_partials < 1 || n_partials > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (n_partials < 1 || !fits_launch(n_partials, kProbeThreads)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(read_probe_kernel, dim3(static_cast<unsigned>(n_partials)),
                      dim3(kProbeThreads), 0, stream, static_cast<const float4*>(buf), bytes / 16,
                      partials);

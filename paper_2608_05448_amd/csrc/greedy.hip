@@ -437,7 +437,7 @@ __global__ __launch_bounds__(256) void greedy_finalize_kernel(GreedyArgs a) {
 }  // namespace
 
 hipError_t launch_sample_greedy(const GreedyArgs& a, hipStream_t stream) {
-  if (a.blk.B > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!fits_launch(a.blk.B, 64)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(greedy_sample_kernel, dim3(static_cast<unsigned>(a.blk.B)), dim3(64), 0,
                      stream, a);
   return hipGetLastError();
@@ -445,8 +445,9 @@ hipError_t launch_sample_greedy(const GreedyArgs& a, hipStream_t stream) {
 
 hipError_t launch_verify_greedy(const GreedyArgs& a, hipStream_t stream) {
   const int64_t B = a.blk.B;
-  if (B > 0x7fffffff) return hipErrorInvalidConfiguration;
-  if (a.blk.K <= kGreedyStageK && a.blk.K * a.blk.R <= kGreedyStageKR)
+  const bool parallel = a.blk.K <= kGreedyStageK && a.blk.K * a.blk.R <= kGreedyStageKR;
+  if (!fits_launch(B, parallel || !a.trajectory ? 256 : 64)) return hipErrorInvalidConfiguration;
+  if (parallel)
     hipLaunchKernelGGL(greedy_chain_parallel_kernel, dim3(static_cast<unsigned>(B)), dim3(256), 0,
                        stream, a);
   else

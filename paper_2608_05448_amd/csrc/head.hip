@@ -1707,7 +1707,7 @@ hipError_t launch_head_train(const HeadTrainArgs& a, bool grad, hipStream_t stre
 
 hipError_t launch_argmax_clear(uint64_t* amax, int64_t M, hipStream_t stream) {
   const int64_t zb = (M + 255) / 256;
-  if (zb > kMaxThreads / 256) return hipErrorInvalidConfiguration;
+  if (!fits_launch(zb, 256)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(zero_u64_kernel, dim3(static_cast<unsigned>(zb)), dim3(256), 0, stream, amax, M);
   return hipGetLastError();
 }
@@ -1817,7 +1817,7 @@ template <class C>
 hipError_t launch_expand_cfg(const ExpandArgs& a, int64_t N, hipStream_t stream) {
   const int dm = static_cast<int>((a.M + C::BM - 1) / C::BM);
   const int64_t dwg = ((N + C::BV - 1) / C::BV) * dm;
-  if (dwg > 0x7fffffff || a.d % C::BK != 0) return hipErrorInvalidConfiguration;
+  if (!fits_launch(dwg, C::kThreads) || a.d % C::BK != 0) return hipErrorInvalidConfiguration;
   EpiArgs ea{};
   ea.out = static_cast<__bf16*>(a.out);
   ea.bias = static_cast<const __bf16*>(a.c);
@@ -1835,7 +1835,7 @@ template <class C>
 hipError_t launch_expand_rs(const ExpandArgs& a, int64_t N, hipStream_t stream) {
   const int dm = static_cast<int>((a.M + C::BM - 1) / C::BM);
   const int64_t dwg = ((N + C::BV - 1) / C::BV) * dm;
-  if (dwg > 0x7fffffff || a.d % C::BK != 0) return hipErrorInvalidConfiguration;
+  if (!fits_launch(dwg, C::kThreads) || a.d % C::BK != 0) return hipErrorInvalidConfiguration;
   EpiArgs ea{};
   ea.out = static_cast<__bf16*>(a.out);
   ea.bias = static_cast<const __bf16*>(a.c);
@@ -1893,7 +1893,7 @@ hipError_t launch_expand(const ExpandArgs& a, hipStream_t stream) {
 }
 
 hipError_t launch_prior_head(const PriorHeadArgs& a, hipStream_t stream) {
-  if (a.B > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!fits_launch(a.B, 256)) return hipErrorInvalidConfiguration;
   const dim3 grid(static_cast<unsigned>(a.B), static_cast<unsigned>(a.R));
   const __bf16* ha = static_cast<const __bf16*>(a.h_anchor);
   const __bf16* U = static_cast<const __bf16*>(a.U);

@@ -405,7 +405,8 @@ struct DrawLayout {
 };
 inline size_t draw_row_bytes(int64_t V) { return DrawLayout(draw_segments(V)).total; }
 
-constexpr int64_t kMaxThreads = 0xffffffffll;     // of a launch
+constexpr int64_t kMaxThreads = 0xffffffffll;     // of a launch; what is more is dropped without an error
+inline bool fits_launch(int64_t blocks, int threads) { return blocks <= kMaxThreads / threads; }
 constexpr int64_t kMaxTrainRows = (1 << 24) - 1;  // a workgroup of 256 each
 
 constexpr int64_t kMaxTensors = int64_t(1) << 20;  // of a norm or clipping call

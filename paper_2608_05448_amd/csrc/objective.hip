@@ -203,9 +203,10 @@ __global__ __launch_bounds__(256) void objective_parallel_kernel(ObjectiveArgs a
 }  // namespace
 
 hipError_t launch_objective(const ObjectiveArgs& a, hipStream_t stream) {
-  if (a.blk.B > 0x7fffffff) return hipErrorInvalidConfiguration;
   // Blocks whose gathers fit the parallel form's LDS; the walk only for longer ones.
-  if (a.blk.K * a.blk.R <= kObjMaxKR && a.blk.K <= kObjMaxK)
+  const bool parallel = a.blk.K * a.blk.R <= kObjMaxKR && a.blk.K <= kObjMaxK;
+  if (!fits_launch(a.blk.B, parallel ? 256 : 64)) return hipErrorInvalidConfiguration;
+  if (parallel)
     hipLaunchKernelGGL(objective_parallel_kernel, dim3(static_cast<unsigned>(a.blk.B)), dim3(256),
                        0, stream, a);
   else

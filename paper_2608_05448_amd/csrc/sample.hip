@@ -59,7 +59,7 @@ __global__ __launch_bounds__(256) void sample_kernel(SampleArgs a) {
 
 hipError_t launch_sample(const SampleArgs& a, hipStream_t stream) {
   const int64_t npos = a.blk.B * a.blk.K;
-  if (npos > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!fits_launch(npos, 256)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(sample_kernel, dim3(static_cast<unsigned>(npos)), dim3(256), 0, stream, a);
   return hipGetLastError();
 }

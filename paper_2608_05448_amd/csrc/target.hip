@@ -1735,20 +1735,22 @@ __global__ __launch_bounds__(kFT) void determinism_mean_kernel(DeterminismArgs a
 }  // namespace
 
 hipError_t launch_filter(const FilterArgs& a, hipStream_t stream) {
-  if (a.N > 0x7fffffff / 4) return hipErrorInvalidConfiguration;
-  const dim3 rows(static_cast<unsigned>(a.N));
   const bool k_off = a.top_k == 0 || a.top_k >= a.V;
   const bool nucleus = a.temperature > 0.0f && k_off && a.top_p < 1.0f;
   const int segs = static_cast<int>(n_segs(a.V));
-  // Split rows: with a workspace, from two segments on (the whole grids below stay in range).
+  const int parts = static_cast<int>((a.V + kMassElems - 1) / kMassElems);
+  const bool short_rows = a.temperature > 0.0f && k_off && !nucleus && segs <= kRowSegs;
+  if (!fits_launch(a.N, short_rows ? kSegT : kFT)) return hipErrorInvalidConfiguration;
+  const dim3 rows(static_cast<unsigned>(a.N));
+  // Split rows: with a workspace, from two segments on, where every grid below fits a launch.
   const bool split = a.row_ws && a.cuts && a.temperature > 0.0f && a.V >= kSplitMinV &&
-                     a.N <= 0x7fffffff / (segs > 16 ? segs : 16);
+                     fits_launch(a.N * segs, kSegT) && fits_launch(a.N * parts, kFT) &&
+                     fits_launch(a.N * 16, kTopThreads);
   auto grid = [&](int per_row) { return dim3(static_cast<unsigned>(a.N * per_row)); };
   hipError_t e;
-  if (a.temperature > 0.0f && k_off && !nucleus && segs <= kRowSegs) {
+  if (short_rows) {
     hipLaunchKernelGGL(filter_scale_rows_kernel, rows, dim3(kSegT), 0, stream, a, segs);
   } else if (split && nucleus && a.V >= kSplitMinNucleus) {
-    const int parts = static_cast<int>((a.V + kMassElems - 1) / kMassElems);
     hipLaunchKernelGGL(nucleus_max_kernel, grid(segs), dim3(kSegT), 0, stream, a, segs);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(nucleus_mass_kernel, grid(parts), dim3(kFT), 0, stream, a, parts, segs);
@@ -1780,7 +1782,7 @@ hipError_t launch_filter(const FilterArgs& a, hipStream_t stream) {
 
 hipError_t launch_determinism(const DeterminismArgs& a, hipStream_t stream) {
   const int64_t blocks = (a.M + 255) / 256;
-  if (blocks > 0x7fffffff) return hipErrorInvalidConfiguration;
+  if (!fits_launch(blocks, 256)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL(determinism_terms_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0,
                      stream, a);
   hipError_t e = hipGetLastError();

@@ -937,21 +937,26 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
   const int64_t B = a.blk.B;
   const int64_t npos = B * a.blk.K;
   const int nchunk = n_chunks(a.blk.nT);
-  if (npos > 0x7fffffff) return hipErrorInvalidConfiguration;
-  if (a.blk.K * a.blk.R <= kChainMaxKR && a.blk.K <= kChainMaxK)
+  const bool want_beta = a.beta || a.exp_len;
+  const bool stream_path = want_beta && !a.trajectory && a.blk.V >= 4;  // a row holds a group of four
+  const int rows = static_cast<int>(a.blk.K) + (!a.trajectory && a.Kp == a.blk.K + 1 ? 1 : 0);
+  const bool parallel = a.blk.K * a.blk.R <= kChainMaxKR && a.blk.K <= kChainMaxK;
+  // Whether every launch below fits, before the first one (the streams' grids are checked where they are known:
+  // rows B workgroups are the least of them).
+  if (!fits_launch(B, parallel || want_beta || !a.trajectory ? 256 : 64) ||
+      (want_beta && !fits_launch(stream_path ? rows * B : npos, 256)))
+    return hipErrorInvalidConfiguration;
+  if (parallel)
     hipLaunchKernelGGL(chain_parallel_kernel, dim3(static_cast<unsigned>(B)), dim3(256), 0, stream,
                        a);
   else
     hipLaunchKernelGGL(chain_kernel, dim3(static_cast<unsigned>(B)), dim3(64), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const bool want_beta = a.beta || a.exp_len;
-  const bool stream_path = want_beta && !a.trajectory && a.blk.V >= 4;  // a row holds a group of four
   const int64_t R = a.blk.R;  // the template argument of the streams below: R, or 0
   const int rt = R <= 8 || R == 16 ? static_cast<int>(R) : 0;
   const int nchunk_s = (a.blk.nT + stream_tiles(rt) - 1) / stream_tiles(rt);
   const int nchunk_f = stream_path ? nchunk_s : nchunk;  // the finalisation's partials per position
-  const int rows = static_cast<int>(a.blk.K) + (!a.trajectory && a.Kp == a.blk.K + 1 ? 1 : 0);
   if (stream_path && a.blk.nT > kWideMinTiles && rows * B * nchunk <= kWideMaxGroups) {
     const dim3 grid(static_cast<unsigned>(rows * B * nchunk_s));
 #define DBL_WIDE(r)                                                                             \
@@ -980,7 +985,7 @@ hipError_t launch_verify(const VerifyArgs& a, hipStream_t stream) {
     const int cpw = stream_multi_chunk(rt) && rows * B * cw_many >= kStreamMinGroups
                         ? kStreamChunksSmallR : 1;
     const int64_t nwg = static_cast<int64_t>(rows) * B * ((nchunk_s + cpw - 1) / cpw);
-    if (nwg > 0x7fffffff) return hipErrorInvalidConfiguration;
+    if (!fits_launch(nwg, 256)) return hipErrorInvalidConfiguration;
     const dim3 grid(static_cast<unsigned>(nwg));
     switch (rt) {
       case 1: hipLaunchKernelGGL(verify_stream_kernel<1>, grid, dim3(256), 0, stream, a, nchunk_s, cpw); break;
