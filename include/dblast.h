@@ -523,12 +523,13 @@ int64_t dbl_mx_row(int64_t d);
 
 /*
  * dbl_mx_quantize - rows x [M, d] of type dt in microscaled form.
- *   M >= 0, 1 <= d <= 2^20;  dt DBL_BF16 or DBL_F32;  bits 4 or 8
+ *   0 <= M < 2^40, 1 <= d <= 2^20;  dt DBL_BF16 or DBL_F32;  bits 4 or 8
  *   codes, scales   out, as above, padding included
  * dbl_mx_dequantize - the values of microscaled rows as type dt, rounded once: out [M, d]. (What
  * dbl_mx_quantize gave is exact in either type, as long as it is in the type's range.)
  * The outputs may overlap neither each other nor an input. Errors: DBL_EINVAL for null, misaligned or
- * overlapping pointers or other bits; DBL_EDTYPE; DBL_ESHAPE.
+ * overlapping pointers or other bits; DBL_EDTYPE; DBL_ESHAPE; DBL_EHIP (where a launch would need 2^32
+ * threads).
  */
 dbl_status dbl_mx_quantize(int64_t M, int64_t d, int dt, const void* x, int bits, void* codes,
                            uint8_t* scales, void* stream);
@@ -539,7 +540,8 @@ dbl_status dbl_mx_dequantize(int64_t M, int64_t d, int bits, const void* codes, 
  * dbl_add_rmsnorm_mx - the norm in front of the head (or of the next projection), quantised:
  *     sum = x + residual,   y = sum / sqrt(mean_j sum_j^2 + eps) * weight,
  * the addition in fp32 and rounded once to dt, and the norm taken of that rounded sum (what later layers
- * see), in binary64; y is rounded once, to its codes.
+ * see), in binary64; y is rounded once, to its codes. (A finite y past fp32's range is taken as fp32's largest
+ * number where it is coded, and is infinite in an fp32 y.)
  *   x, residual   [M, d] of type dt; residual may be NULL (then sum is x, and is not written)
  *   weight        [d] of type dt;  eps >= 0, finite
  *   sum           out [M, d] of type dt, NULL if it is not wanted or there is no residual; may be x or
@@ -547,7 +549,8 @@ dbl_status dbl_mx_dequantize(int64_t M, int64_t d, int bits, const void* codes, 
  *   bits, codes, scales   y in microscaled form, as dbl_mx_quantize
  *   y             out [M, d] of type dt or NULL: y itself, rounded once
  * Otherwise the outputs may overlap neither each other nor an input. A row of zeros with eps = 0 gives NaN.
- * Errors: as dbl_mx_quantize, and DBL_EINVAL for eps < 0 or not finite, or sum without residual.
+ * Errors: as dbl_mx_quantize (2^32 threads: 2^24 rows of more than 512 values, 2^26 of fewer), and DBL_EINVAL
+ * for eps < 0 or not finite, or sum without residual.
  */
 dbl_status dbl_add_rmsnorm_mx(int64_t M, int64_t d, int dt, const void* x, const void* residual,
                               const void* weight, float eps, void* sum, int bits, void* codes,
@@ -557,13 +560,15 @@ dbl_status dbl_add_rmsnorm_mx(int64_t M, int64_t d, int dt, const void* x, const
  * dbl_mx_matmul - logits of microscaled states against a head in microscaled 4 bits,
  *     logits[m, v] = sum_j h[m, j] w[v, j],  m < M, v < V,
  * over the values that the codes stand for, summed in fp32 and rounded once to the type of the logits.
- * With fp32 logits no product is cut; with bf16 logits and 8-bit states, products are cut at 2^-13 of the
- * largest in their group of eight (below the rounding of the result). A row's logits do not depend on the
- * other rows.
+ * With fp32 logits no product is cut. With bf16 logits and 8-bit states, each product is cut at 2^-13 of the
+ * power of two of the largest in its group of eight consecutive values: less than the rounding of a logit of
+ * the size of its products, but a logit that is small by cancellation can be off by more than its own
+ * rounding, up to 7 2^-12 sum over the groups of (largest |h| times largest |w|). A row's logits do not depend
+ * on the other rows.
  *   bits   of h, 4 or 8;  h, hs   [M, dp] states;  w, ws   [V, dp] 4-bit head
  *   dt     DBL_F32 or DBL_BF16: type of logits, out [M, V]
- * No workspace. M >= 0, 1 <= V < 2^24, 1 <= d <= 2^20. Errors: DBL_EINVAL, DBL_EDTYPE, DBL_ESHAPE, DBL_EHIP (where a
- * launch would need 2^32 threads).
+ * No workspace. 0 <= M < 2^40, 1 <= V < 2^24, 1 <= d <= 2^20. Errors: DBL_EINVAL, DBL_EDTYPE, DBL_ESHAPE, DBL_EHIP
+ * (where a launch would need 2^32 threads).
  *
  * dbl_mx_head_logprobs - dbl_head_logprobs for microscaled operands: the same outputs (the two-level form
  * that dbl_sample_block, dbl_verify_block and the others read) of the same logits as dbl_mx_matmul's in

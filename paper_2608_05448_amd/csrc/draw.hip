@@ -17,11 +17,18 @@
 //   find    (only where there are filters) a workgroup per row finds the cut's bound, as follows
 //   cut     (only where there are filters) lists the ids that the cut goes through, and sums by segment what is
 //           surely kept. Top-k: the k-th largest of the maxima of 128 ids is a bound from below for the k-th
-//           largest id, so that what reaches it holds all that is kept (about k ids) and nothing else
-//           is looked at. Otherwise: the bin that the cut falls into is listed, what is above it summed
+//           largest id, so that what reaches it holds all that is kept and nothing else is looked at: about k ids for
+//           small k and large logits at random ids, more the nearer k is to the number of groups (k = 1000 of 1187:
+//           2200, from 1150 on past the list) or the more large logits share groups (ids in the order of their
+//           frequency: 2300 at k = 50, 4600 at 100). Otherwise: the bin that the cut falls into is listed, what is
+//           above it summed
 //   finish  a workgroup per row: sorts the list, finds the exact cut and draws. Rows whose list is
-//           longer than kListMost (many equal logits), or with a large top-k and top-p at once, are selected by
-//           radix over their order-preserving keys here
+//           longer than kListMost, or with a top-k past kListMost / 2 and top-p at once, are selected by
+//           radix over their order-preserving keys here, about ten reads of the row by that one workgroup
+// Long lists are not rare: a bf16 number in the tail of a nucleus may have more than kListMost ids (V = 151,936, of
+// rows like Zipf's law 11% at a temperature of 0.7 and 17% at 1 under top_p = 0.95), and k and the order of the ids
+// make them as above. Such a row costs 0.5 to 0.6 ms where others take 31 us alone, and 272 rows with some of
+// them 1.0 ms (bf16 nucleus; fp32 167 us) to 1.15 (top-k 100 to 1187 of ids in order; 101 us for 50 of spread ids).
 // 272 rows of 151,936 ids under parameters of their own 133 us (top 38, bins 28, find 9, cut 31, finish 29; reading them
 // once takes 24.5), one under a nucleus 31. A weight costs 33 vector operations, which bounds bins and cut.
 #include <hip/hip_runtime.h>

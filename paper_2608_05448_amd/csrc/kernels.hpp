@@ -375,7 +375,7 @@ struct DrawArgs {
   float* logprob;       // [N]
   char* ws;
 };
-// The draw's rows are split into segments of this many ids; a workgroup each.
+// The draw's rows are split into segments of this many ids, and the segments of a row among its workgroups (parts).
 constexpr int kDrawSeg = 4096;
 // Segments of a row: up to 7 ids more than V, where a row starts inside a 16-byte word.
 inline int64_t draw_segments(int64_t V) { return (V + 7 + kDrawSeg - 1) / kDrawSeg; }
@@ -389,8 +389,8 @@ struct DrawState {       // of a row
   uint32_t unused[9];
 };
 static_assert(sizeof(DrawState) == 64, "the row's arrays follow it");
-// A row's workspace, for G segments: the state; by segment the maximum, the sum and the maxima of 128 ids
-// each; the list; the bins' masses and counts.
+// A row's workspace, for G segments: the state; by part (G at most) the maximum; by segment the sum and the maxima
+// of 128 ids each; the list; the bins' masses and counts.
 struct DrawLayout {
   size_t top, sum, maxima, list, mass, count, total;
   __host__ __device__ explicit DrawLayout(int64_t G) {
